@@ -264,6 +264,74 @@ int lsp_reset_counters(lsp_ctx* ctx);
 int lsp_linear_static(const void* A, const void* W, void* out, int M, int N, int K, void* cuda_stream, char* err,
                       size_t err_len);
 
+/* ---- Paged key-value cache -------------------------------------------------------------------------------------
+ * (No counterpart in the paper, whose cache is contiguous per sequence: for serving many sequences of unlike lengths from one
+ * pool, and for bounding the committed prefix.)  One layer's keys and values in pages of page_size rows ("slots"); slot j of
+ * sequence b is row j % page_size of page page_table[b * max_pages + j / page_size].  A decoder's own cache plane is the special
+ * case without a table.  The calls need no context, allocate nothing, enqueue on cuda_stream (a cudaStream_t; NULL = default
+ * stream) of the current device and return; they may be captured into a CUDA graph.  Lengths and tables are device memory, read
+ * when the kernels run.  What only the device sees goes to the status word: bit 1 = a length outside [0, max_pages * page_size],
+ * or an append past it (clamped); bit 2 = a table entry outside [0, n_pages) for a slot in use (the slot is not read or written and gets
+ * no weight; a pair of slots of an eviction is not moved); bit 4 = row offsets that descend, leave [0, n_rows] or span more
+ * than max_rows (that sequence has no rows then).  Nothing outside the given buffers is touched in any of these cases, and the
+ * other sequences' results hold.  err, err_len: optional host buffer for the message of a failing call.
+ * Limits: head_dim 64 or 128, batch <= 1024, n_kv_heads <= 1024, max_pages * page_size <= 2^20, every pointer and stride of T a
+ * multiple of 16 bytes. */
+typedef struct {
+  void *k, *v;                 /* device: element (page, row, head, i) at page * page_stride + row * row_stride + head * head_stride + i */
+  const int32_t* page_table;   /* device [batch][max_pages]; NULL: page p of sequence b is b * max_pages + p */
+  int32_t* status;             /* device word that collects the bits above, cleared by the caller; or NULL */
+  long long page_stride, row_stride, head_stride; /* elements */
+  int n_pages, page_size, max_pages, batch, n_kv_heads, head_dim, dtype; /* dtype: 0 = fp32, 1 = bf16 */
+} lsp_paged_kv;
+
+/* Writes new rows behind the cached ones (AppendToCache for pages): row i of sequence b to slot lens[b] + i.
+ *   k_new, v_new   device, packed rows [n_rows] ld_new elements apart, n_kv_heads * head_dim each: sequence b's rows are
+ *                  row_off[b] .. row_off[b + 1]  (row_off: device [batch + 1]; NULL: max_rows rows for every sequence, n_rows = batch * max_rows)
+ *   max_rows       upper bound of a sequence's rows
+ *   lens, lens_out device [batch]; lens_out[b] = lens[b] + rows.  Outputs must not overlap inputs (two buffers, in turn).
+ *   weights, pos   device [batch][n_kv_heads][max_pages * page_size] or NULL: set to 0 and to the row's position seen[b] + i
+ *                  (seen NULL: the slot) in the new slots
+ *   seen, seen_out device [batch] or both NULL: positions so far, which after an eviction are more than the slots; seen_out = seen + rows
+ * The pages written to must belong to one sequence each. */
+int lsp_paged_append(const lsp_paged_kv* kv, const void* k_new, const void* v_new, long long ld_new, const int32_t* lens,
+                     const int32_t* row_off, int max_rows, int n_rows, int32_t* lens_out, float* weights, int32_t* pos,
+                     const int32_t* seen, int32_t* seen_out, void* cuda_stream, char* err, size_t err_len);
+
+/* Attention of one new row per sequence, or a few, over its lens[b] slots, every row over all of them (the new rows' own keys are
+ * appended first):
+ *   out[r, h] = sum_j softmax_j(scale q[r, h] . k_j) v_j        query head h reads KV head h / (n_heads / n_kv_heads)
+ *   lse[r, h] = ln sum_j exp(scale q[r, h] . k_j)               device [n_rows][n_heads], or NULL
+ *   weights_out[b, g, j] = weights_in[b, g, j] + sum over the sequence's rows r and the group's heads h of the softmax weight of slot j
+ *                                                               device [batch][n_kv_heads][max_pages * page_size], or NULL; weights_in NULL: 0;
+ *                                                               may be the same array; slots behind lens[b] are not written
+ * A row over no slot (lens[b] = 0), or whose scores are all -inf, gets 0 and lse -inf.  q, out: packed rows as for the append, ldq and ldo
+ * elements apart.  The slots are split over the device and the parts joined in a fixed order: the same inputs give the same bits.
+ * Accumulation in fp32; bf16 softmax weights enter the product with V as a sum of two.  Meant for up to some dozens of (row, head)
+ * pairs per KV head; a tile of 16 of them reads the cache once.
+ * workspace: device, 256-byte aligned, lsp_paged_attention_workspace() bytes (for weights it holds the scores), uninitialised; calls that share
+ * one must not overlap on the device. */
+size_t lsp_paged_attention_workspace(const lsp_paged_kv* kv, int n_heads, int n_rows, int with_weights);
+int lsp_paged_attention(const lsp_paged_kv* kv, const void* q, long long ldq, int n_heads, const int32_t* lens,
+                        const int32_t* row_off, int max_rows, int n_rows, float scale, void* out, long long ldo, float* lse,
+                        const float* weights_in, float* weights_out, void* workspace, size_t workspace_bytes,
+                        void* cuda_stream, char* err, size_t err_len);
+
+/* Thins every sequence of more than budget slots to budget, per KV head: kept are the slots of positions < n_sink or >= seen[b] - n_recent
+ * (n_sink + n_recent <= budget), and of the others the heaviest; ties: the lower position; NaN is lighter than any weight.
+ * Kept slots at or behind the budget move into the freed ones ahead of it (the i-th to the i-th): their K and V rows in place, every
+ * slot's weight and position to weights_out and pos_out.  Which slot holds a key carries no meaning for attention (keys are
+ * rotated already); pos_out says which position it is, per KV head.  Sequences of at most budget slots keep theirs.
+ *   weights, pos        device [batch][n_kv_heads][max_pages * page_size]; pos NULL: the slot (pos_out may be NULL then)
+ *   lens, seen          device [batch]; seen NULL: lens
+ *   weights_out, pos_out, lens_out   as the inputs, not overlapping them; lens_out = min(lens, budget); slots behind it are not written
+ * Pages behind ceil(lens_out / page_size) are free afterwards.  The pages of a sequence that is thinned must belong to it alone.
+ * workspace: as above, lsp_paged_evict_workspace() bytes. */
+size_t lsp_paged_evict_workspace(const lsp_paged_kv* kv, int budget);
+int lsp_paged_evict(const lsp_paged_kv* kv, const float* weights, const int32_t* pos, const int32_t* lens, const int32_t* seen,
+                    int budget, int n_sink, int n_recent, float* weights_out, int32_t* pos_out, int32_t* lens_out,
+                    void* workspace, size_t workspace_bytes, void* cuda_stream, char* err, size_t err_len);
+
 const char* lsp_last_error(const lsp_ctx* ctx);
 int lsp_destroy(lsp_ctx* ctx);
 

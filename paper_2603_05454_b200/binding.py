@@ -14,11 +14,13 @@ _LIB_PATH = os.environ.get("LSP_LIB") or os.path.join(_HERE, "liblsp_b200.so")  
 
 FLAG_SNAPPED, FLAG_FALLBACK, FLAG_RANGE_UNACHIEVABLE = 1, 2, 4
 FLAG_RUN_TO_END, FLAG_NEAR_THRESHOLD, FLAG_NEAR_TIE = 8, 16, 32
+PAGED_BAD_LEN, PAGED_BAD_PAGE, PAGED_BAD_ROWS = 1, 2, 4        # bits of a paged cache's status word
 
 EXPORTS = ["lsp_workspace_bytes", "lsp_kv_cache_bytes", "lsp_init", "lsp_set_sched", "lsp_set_option",
            "lsp_begin", "lsp_denoise_step", "lsp_commit", "lsp_generate", "lsp_generate_host", "lsp_active", "lsp_score_rows",
            "lsp_get_scores", "lsp_head_scan", "lsp_scan", "lsp_op_linear", "lsp_op_attention", "lsp_last_timing", "lsp_get_counters", "lsp_reset_counters",
-           "lsp_linear_static", "lsp_last_error", "lsp_destroy"]
+           "lsp_linear_static", "lsp_paged_append", "lsp_paged_attention_workspace", "lsp_paged_attention",
+           "lsp_paged_evict_workspace", "lsp_paged_evict", "lsp_last_error", "lsp_destroy"]
 
 
 class LSPError(RuntimeError):
@@ -46,6 +48,12 @@ class WeightsC(C.Structure):
 class StepRec(C.Structure):
     _fields_ = [("step", C.c_int), ("n_before", C.c_int), ("rows", C.c_int), ("l_run", C.c_int), ("l_commit", C.c_int),
                 ("tau_used", C.c_float), ("flags", C.c_uint), ("ms", C.c_float), ("flips", C.c_int), ("flip_base", C.c_int)]
+
+
+class PagedKV(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_table", C.c_void_p), ("status", C.c_void_p),
+                ("page_stride", C.c_longlong), ("row_stride", C.c_longlong), ("head_stride", C.c_longlong)] + \
+               [(n, C.c_int) for n in ("n_pages", "page_size", "max_pages", "batch", "n_kv_heads", "head_dim", "dtype")]
 
 
 def _load():
@@ -82,6 +90,14 @@ def _load():
     l.lsp_reset_counters.argtypes = [C.c_void_p]
     l.lsp_linear_static.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_char_p,
                                     C.c_size_t]
+    pkv, vp, i, ll, sz, cs = C.POINTER(PagedKV), C.c_void_p, C.c_int, C.c_longlong, C.c_size_t, C.c_char_p
+    l.lsp_paged_append.argtypes = [pkv, vp, vp, ll, vp, vp, i, i, vp, vp, vp, vp, vp, vp, cs, sz]
+    l.lsp_paged_attention_workspace.restype = sz
+    l.lsp_paged_attention_workspace.argtypes = [pkv, i, i, i]
+    l.lsp_paged_attention.argtypes = [pkv, vp, ll, i, vp, vp, i, i, C.c_float, vp, ll, vp, vp, vp, vp, sz, vp, cs, sz]
+    l.lsp_paged_evict_workspace.restype = sz
+    l.lsp_paged_evict_workspace.argtypes = [pkv, i]
+    l.lsp_paged_evict.argtypes = [pkv, vp, vp, vp, vp, i, i, i, vp, vp, vp, vp, sz, vp, cs, sz]
     l.lsp_last_error.restype = C.c_char_p
     l.lsp_last_error.argtypes = [C.c_void_p]
     l.lsp_destroy.argtypes = [C.c_void_p]
@@ -347,6 +363,149 @@ def linear_static(A: torch.Tensor, W: torch.Tensor, out: torch.Tensor, stream=No
     if rc != 0:
         raise LSPError(rc, buf.value.decode())
     return out
+
+
+class PagedKVCache:
+    """One layer's keys and values in pages (lsp_paged_*): append, attention of new rows, eviction by gathered weight.
+
+    k_pool, v_pool: [n_pages, page_size, n_kv_heads, head_dim] CUDA tensors (bfloat16 or float32) with the same strides, heads
+    contiguous; any view with 16-byte strides will do, a decoder's own planes among them.  page_table: int32 CUDA tensor [batch, max_pages],
+    contiguous; without it page p of sequence b is page b * max_pages + p (batch then tells max_pages = n_pages // batch).
+    All tensors are borrowed; page_table may be rewritten between calls.  The object owns the workspace (for any eviction, and for attention of
+    at most n_rows packed rows, by default max_rows for every sequence; with `weights` for attention that gathers them) and the status
+    word that check() reads.  Calls of one object must not overlap on the device: give each stream, and each captured graph that may run
+    beside others, an object of its own over the same pools.  Every call enqueues on the current stream of the pools' device, or on `stream`.
+    """
+
+    def __init__(self, k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: Optional[torch.Tensor] = None, *, n_heads: int,
+                 batch: Optional[int] = None, max_rows: int = 1, n_rows: Optional[int] = None, weights: bool = False):
+        if k_pool.dim() != 4 or v_pool.shape != k_pool.shape or v_pool.stride() != k_pool.stride() or v_pool.dtype != k_pool.dtype:
+            raise ValueError("k_pool and v_pool need one shape [n_pages, page_size, n_kv_heads, head_dim], one type and one layout")
+        if not (k_pool.is_cuda and v_pool.device == k_pool.device) or k_pool.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("the pools must be float32 or bfloat16 tensors of one CUDA device")
+        if k_pool.shape[3] > 1 and k_pool.stride(3) != 1:
+            raise ValueError("the elements of a head must be contiguous")
+        n_pages, page_size, n_kv, dh = k_pool.shape
+        if page_table is not None:
+            if page_table.dim() != 2:
+                raise ValueError("page_table must be [batch, max_pages]")
+            self._tensor("page_table", page_table, torch.int32, tuple(page_table.shape), k_pool.device)
+            self.batch, self.max_pages = page_table.shape
+            if batch not in (None, self.batch):
+                raise ValueError(f"page_table has {self.batch} sequences, not {batch}")
+        else:
+            self.batch = batch or 1
+            self.max_pages = n_pages // self.batch
+        self.device, self.dtype = k_pool.device, k_pool.dtype
+        self.n_heads, self.n_kv_heads, self.head_dim = n_heads, n_kv, dh
+        self.max_rows = max_rows
+        self.capacity = self.max_pages * page_size
+        self.k_pool, self.v_pool, self.page_table = k_pool, v_pool, page_table
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._kv = PagedKV(k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr() if page_table is not None else None,
+                           self.status.data_ptr(), k_pool.stride(0), k_pool.stride(1), k_pool.stride(2), n_pages, page_size,
+                           self.max_pages, self.batch, n_kv, dh, 0 if k_pool.dtype == torch.float32 else 1)
+        self._ref = C.byref(self._kv)
+        self._err = C.create_string_buffer(256)
+        rows = self.batch * max_rows if n_rows is None else n_rows
+        need = lib.lsp_paged_attention_workspace(self._ref, n_heads, rows, int(weights))
+        if need == 0:
+            # the library's own words for what is wrong with the description
+            self._check(lib.lsp_paged_evict(self._ref, None, None, None, None, 1, 0, 0, None, None, None, None, 0, None, self._err, 256))
+        # (an eviction moves most where half of the slots go)
+        need = max(need, lib.lsp_paged_evict_workspace(self._ref, max(1, self.capacity // 2)))
+        self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+
+    @staticmethod
+    def _tensor(name, t, dtype, shape, device):
+        if t.dtype != dtype or tuple(t.shape) != shape or t.device != device or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {list(shape)} on {device}")
+        return t.data_ptr()
+
+    def _opt(self, name, t, dtype, shape):
+        return None if t is None else self._tensor(name, t, dtype, shape, self.device)
+
+    def _rows(self, name, t, width):
+        """Packed rows [n_rows, width], rows any distance apart."""
+        if t.dtype != self.dtype or t.dim() != 2 or t.shape[1] != width or t.device != self.device or (width > 1 and t.stride(1) != 1):
+            raise ValueError(f"{name} must be a {self.dtype} tensor of shape [rows, {width}] on {self.device}, elements of a row contiguous")
+        return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), width))
+
+    def _row_off(self, row_off, n_rows, max_rows):
+        """Pointer to the offsets and the bound of a sequence's rows."""
+        if row_off is not None:
+            return self._tensor("row_off", row_off, torch.int32, (self.batch + 1,), self.device), max_rows or self.max_rows
+        if n_rows % self.batch or n_rows == 0:
+            raise ValueError(f"without row_off every one of the {self.batch} sequences has as many rows: {n_rows} rows do not divide")
+        return None, n_rows // self.batch
+
+    def _check(self, rc):
+        if rc != 0:
+            raise LSPError(rc, self._err.value.decode())
+
+    def _call(self, stream, fn, *args):
+        sptr = torch.cuda.current_stream(self.device).cuda_stream if stream is None else stream.cuda_stream
+        if torch.cuda.current_device() == self.device.index:
+            rc = fn(self._ref, *args, sptr, self._err, 256)
+        else:
+            with torch.cuda.device(self.device):
+                rc = fn(self._ref, *args, sptr, self._err, 256)
+        self._check(rc)
+
+    def append(self, k_new: torch.Tensor, v_new: torch.Tensor, lens: torch.Tensor, lens_out: torch.Tensor, *, row_off=None,
+               max_rows: Optional[int] = None, weights=None, pos=None, seen=None, seen_out=None, stream=None):
+        """Writes packed rows k_new, v_new [n_rows, n_kv_heads * head_dim] behind the lens[b] cached ones (lsp_paged_append)."""
+        width = self.n_kv_heads * self.head_dim
+        kp, ld = self._rows("k_new", k_new, width)
+        vp, ldv = self._rows("v_new", v_new, width)
+        if v_new.shape != k_new.shape or ldv != ld:
+            raise ValueError("k_new and v_new need one shape and one row stride")
+        n = k_new.shape[0]
+        off, most = self._row_off(row_off, n, max_rows)
+        b, per_slot = (self.batch,), (self.batch, self.n_kv_heads, self.capacity)
+        self._call(stream, lib.lsp_paged_append, kp, vp, ld, self._opt("lens", lens, torch.int32, b), off, most, n,
+                   self._opt("lens_out", lens_out, torch.int32, b), self._opt("weights", weights, torch.float32, per_slot),
+                   self._opt("pos", pos, torch.int32, per_slot), self._opt("seen", seen, torch.int32, b),
+                   self._opt("seen_out", seen_out, torch.int32, b))
+        return lens_out
+
+    def attention(self, q: torch.Tensor, lens: torch.Tensor, out: torch.Tensor, *, row_off=None, max_rows: Optional[int] = None,
+                  scale: Optional[float] = None, lse=None, weights_in=None, weights_out=None, stream=None):
+        """Attention of packed rows q [n_rows, n_heads * head_dim] over their sequences' slots (lsp_paged_attention); scale: 1 / sqrt(head_dim)."""
+        width = self.n_heads * self.head_dim
+        qp, ldq = self._rows("q", q, width)
+        op, ldo = self._rows("out", out, width)
+        n = q.shape[0]
+        if out.shape[0] != n:
+            raise ValueError(f"q has {n} rows, out {out.shape[0]}")
+        off, most = self._row_off(row_off, n, max_rows)
+        per_slot = (self.batch, self.n_kv_heads, self.capacity)
+        self._call(stream, lib.lsp_paged_attention, qp, ldq, self.n_heads, self._opt("lens", lens, torch.int32, (self.batch,)), off, most, n,
+                   self.head_dim ** -0.5 if scale is None else scale, op, ldo, self._opt("lse", lse, torch.float32, (n, self.n_heads)),
+                   self._opt("weights_in", weights_in, torch.float32, per_slot), self._opt("weights_out", weights_out, torch.float32, per_slot),
+                   self.workspace.data_ptr(), self.workspace.numel())
+        return out
+
+    def evict(self, weights: torch.Tensor, lens: torch.Tensor, budget: int, weights_out: torch.Tensor, lens_out: torch.Tensor, *,
+              n_sink: int = 0, n_recent: int = 0, pos=None, pos_out=None, seen=None, stream=None):
+        """Thins every sequence to at most budget slots per KV head (lsp_paged_evict)."""
+        b, per_slot = (self.batch,), (self.batch, self.n_kv_heads, self.capacity)
+        self._call(stream, lib.lsp_paged_evict, self._opt("weights", weights, torch.float32, per_slot), self._opt("pos", pos, torch.int32, per_slot),
+                   self._opt("lens", lens, torch.int32, b), self._opt("seen", seen, torch.int32, b), budget, n_sink, n_recent,
+                   self._opt("weights_out", weights_out, torch.float32, per_slot), self._opt("pos_out", pos_out, torch.int32, per_slot),
+                   self._opt("lens_out", lens_out, torch.int32, b), self.workspace.data_ptr(), self.workspace.numel())
+        return lens_out
+
+    def check(self):
+        """Waits for the device and raises LSPError (LSP_ERR_STATE) with the status bits if a call since the last check met lengths, table
+        entries or row offsets out of range; clears them."""
+        torch.cuda.synchronize(self.device)
+        bits = int(self.status.item())
+        if bits:
+            self.status.zero_()
+            words = [w for bit, w in ((PAGED_BAD_LEN, "a length outside the sequence's pages"), (PAGED_BAD_PAGE, "a table entry outside the pool"),
+                                      (PAGED_BAD_ROWS, "row offsets out of range")) if bits & bit]
+            raise LSPError(-4, f"paged cache: {', '.join(words)} (status {bits})")
 
 
 def _rec(r: StepRec):

@@ -6,9 +6,9 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblsp_b200.so")
-SOURCES = ["lsp_api.cu"]
+SOURCES = ["lsp_api.cu", "lsp_paged.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-Xcompiler", "-fPIC", "-shared", "--expt-relaxed-constexpr"]
+              "-Xcompiler", "-fPIC", "-shared", "--expt-relaxed-constexpr", "--threads", "2"]
 
 
 def _newest_source_mtime():

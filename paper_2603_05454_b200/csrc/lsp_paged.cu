@@ -1,0 +1,274 @@
+// C ABI of the paged key-value cache (see include/lsp.h for the contract).
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+
+#include "../../include/lsp.h"
+#include "paged_attention.cuh"
+#include "paged_cache.cuh"
+
+using namespace lsp;
+
+namespace {
+
+struct Err {
+  char* buf;
+  size_t len;
+  int fail(int code, const char* fmt, ...) const {
+    if (buf && len) {
+      va_list ap;
+      va_start(ap, fmt);
+      vsnprintf(buf, len, fmt, ap);
+      va_end(ap);
+    }
+    return code;
+  }
+};
+
+size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+
+// What every call checks of the cache's description.
+int check_view(const Err& e, const char* who, const lsp_paged_kv* kv, PagedView* pv) {
+  if (!kv || !kv->k || !kv->v) return e.fail(LSP_ERR_ARG, "%s: NULL cache or pool", who);
+  if (kv->dtype != 0 && kv->dtype != 1) return e.fail(LSP_ERR_ARG, "%s: dtype %d is neither 0 (fp32) nor 1 (bf16)", who, kv->dtype);
+  if (kv->head_dim != 64 && kv->head_dim != 128) return e.fail(LSP_ERR_SHAPE, "%s: head_dim %d is neither 64 nor 128", who, kv->head_dim);
+  if (kv->n_pages < 1 || kv->page_size < 1 || kv->max_pages < 1 || kv->n_kv_heads < 1 || kv->batch < 1)
+    return e.fail(LSP_ERR_ARG, "%s: n_pages, page_size, max_pages, n_kv_heads and batch must be positive", who);
+  if (kv->batch > PA_MAX_BATCH) return e.fail(LSP_ERR_SHAPE, "%s: batch %d exceeds %d", who, kv->batch, PA_MAX_BATCH);
+  if (kv->n_kv_heads > 1024) return e.fail(LSP_ERR_SHAPE, "%s: n_kv_heads %d exceeds 1024", who, kv->n_kv_heads);
+  if ((long long)kv->max_pages * kv->page_size > PE_MAX_CAP)
+    return e.fail(LSP_ERR_SHAPE, "%s: max_pages x page_size = %lld slots exceed %d", who, (long long)kv->max_pages * kv->page_size, PE_MAX_CAP);
+  if (!kv->page_table && (long long)kv->batch * kv->max_pages > kv->n_pages)
+    return e.fail(LSP_ERR_ARG, "%s: without a page table the pool needs batch x max_pages pages", who);
+  const int per16 = kv->dtype == 0 ? 4 : 8;
+  if (kv->page_stride % per16 || kv->row_stride % per16 || kv->head_stride % per16 || ((uintptr_t)kv->k & 15) || ((uintptr_t)kv->v & 15))
+    return e.fail(LSP_ERR_ARG, "%s: pools and their strides must be multiples of 16 bytes", who);
+  if (kv->page_stride < 0 || kv->row_stride < kv->head_dim || kv->head_stride < (kv->n_kv_heads > 1 ? kv->head_dim : 0))
+    return e.fail(LSP_ERR_ARG, "%s: strides smaller than a head", who);
+  if (((uintptr_t)kv->page_table & 3) || ((uintptr_t)kv->status & 3)) return e.fail(LSP_ERR_ARG, "%s: page_table or status misaligned", who);
+  *pv = PagedView{(char*)kv->k, (char*)kv->v, kv->page_table, kv->status, kv->page_stride, kv->row_stride, kv->head_stride,
+                  kv->n_pages, kv->page_size, kv->max_pages, kv->batch, kv->n_kv_heads};
+  return LSP_OK;
+}
+
+int check_rows(const Err& e, const char* who, const lsp_paged_kv* kv, const int32_t* row_off, int max_rows, int n_rows) {
+  if (max_rows < 1 || n_rows < 0) return e.fail(LSP_ERR_ARG, "%s: max_rows %d or n_rows %d", who, max_rows, n_rows);
+  if (!row_off && (long long)kv->batch * max_rows != n_rows)
+    return e.fail(LSP_ERR_ARG, "%s: without row offsets every sequence has max_rows = %d rows: n_rows must be %lld, not %d", who, max_rows,
+                  (long long)kv->batch * max_rows, n_rows);
+  return LSP_OK;
+}
+
+// int32 and float arrays (and the status word) lie on their own boundary
+template <typename... P>
+bool off_boundary(const P*... p) { return (((uintptr_t)p & 3) | ...); }
+
+bool overlap(const void* a, const void* b, size_t bytes_a, size_t bytes_b) {
+  return a && b && (const char*)a < (const char*)b + bytes_b && (const char*)b < (const char*)a + bytes_a;
+}
+
+struct AttnLayout { size_t part_o, part_ml, row_ml, scores, total; };
+AttnLayout attn_layout(const lsp_paged_kv* kv, int n_heads, int n_rows, int with_weights) {
+  AttnLayout L;
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t o = at; at += align256(bytes); return o; };
+  L.part_o = take((size_t)2 * PA_MAX_CTAS * PA_ROWS * kv->head_dim * 4);
+  L.part_ml = take((size_t)2 * PA_MAX_CTAS * PA_ROWS * 8);
+  L.row_ml = take(with_weights ? (size_t)n_rows * n_heads * 8 : 0);
+  L.scores = take(with_weights ? (size_t)n_rows * n_heads * kv->max_pages * kv->page_size * 4 : 0);
+  L.total = at;
+  return L;
+}
+
+long long evict_moves(const lsp_paged_kv* kv, int budget) {
+  const long long cap = (long long)kv->max_pages * kv->page_size;
+  return cap > budget ? std::min<long long>(budget, cap - budget) : 0;
+}
+
+template <typename T, int DH>
+cudaError_t launch_attention(const PagedAttnArgs& a0, int tiles, cudaStream_t stream) {
+  PagedAttnArgs a = a0;
+  void (*kern)(PagedAttnArgs);
+  if constexpr (sizeof(T) == 2) kern = k_paged_attn_mma<DH>;
+  else kern = k_paged_attn_simt<DH>;
+  constexpr int smem = pa_smem_bytes<T, DH>();
+  constexpr int per_sm = 2 * (smem + 1024) <= 228 * 1024 ? 2 : 1;
+  int dev = 0, n_sm = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev);
+  // (the limit belongs to the CUDA context: set with every call)
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  const long long cap = (long long)a.pv.max_pages * a.pv.page;
+  const long long most = (cap + PA_CHUNK - 1) / PA_CHUNK * a.pv.batch * a.pv.hkv * tiles;       // chunks, if every sequence were full
+  a.n_cta = (int)std::min<long long>(most, std::min(per_sm * n_sm, PA_MAX_CTAS));
+  e = launch_k(1, kern, dim3(a.n_cta), dim3(PA_WARPS * 32), (size_t)smem, stream, a);
+  if (e != cudaSuccess) return e;
+  const int rows_tile = std::min(PA_ROWS, a.max_rows * a.group);
+  const int join_blocks = a.pv.batch * a.pv.hkv * tiles * rows_tile;
+  const int key_blocks = a.scores ? (int)((cap + PJ_KEYS - 1) / PJ_KEYS) : 0;
+  return launch_k(1, k_paged_join<T, DH>, dim3(join_blocks + a.pv.batch * a.pv.hkv * key_blocks), dim3(PJ_THREADS),
+                  a.scores ? (size_t)a.max_rows * a.group * 4 : 0, stream, a, tiles, rows_tile, join_blocks, key_blocks);
+}
+
+}  // namespace
+
+extern "C" {
+
+int lsp_paged_append(const lsp_paged_kv* kv, const void* k_new, const void* v_new, long long ld_new, const int32_t* lens, const int32_t* row_off,
+                     int max_rows, int n_rows, int32_t* lens_out, float* weights, int32_t* pos, const int32_t* seen, int32_t* seen_out,
+                     void* cuda_stream, char* err, size_t err_len) {
+  const Err e{err, err_len};
+  const char* who = "lsp_paged_append";
+  PagedAppendArgs a;
+  int rc = check_view(e, who, kv, &a.pv);
+  if (rc) return rc;
+  rc = check_rows(e, who, kv, row_off, max_rows, n_rows);
+  if (rc) return rc;
+  if (!lens || !lens_out || (n_rows > 0 && (!k_new || !v_new))) return e.fail(LSP_ERR_ARG, "%s: NULL pointer", who);
+  if (off_boundary(lens, row_off, lens_out, weights, pos, seen, seen_out)) return e.fail(LSP_ERR_ARG, "%s: misaligned array", who);
+  if ((seen_out != nullptr) != (seen != nullptr)) return e.fail(LSP_ERR_ARG, "%s: seen and seen_out come together", who);
+  const size_t nb = (size_t)kv->batch * 4;
+  if (overlap(lens, lens_out, nb, nb) || overlap(seen, seen_out, nb, nb) || overlap(lens, seen_out, nb, nb) || overlap(seen, lens_out, nb, nb) ||
+      overlap(seen_out, lens_out, nb, nb))
+    return e.fail(LSP_ERR_ARG, "%s: lens_out and seen_out must not overlap what the call reads, nor one another", who);
+  a.esz = kv->dtype == 0 ? 4 : 2;
+  if ((ld_new * a.esz) % 16 || ((uintptr_t)k_new & 15) || ((uintptr_t)v_new & 15) || ld_new < (long long)kv->n_kv_heads * kv->head_dim)
+    return e.fail(LSP_ERR_ARG, "%s: new rows must be 16-byte aligned and at least n_kv_heads x head_dim elements apart", who);
+  a.k_new = (const char*)k_new;
+  a.v_new = (const char*)v_new;
+  a.ld_new = ld_new * a.esz;
+  a.lens = lens;
+  a.row_off = row_off;
+  a.seen = seen;
+  a.max_rows = max_rows;
+  a.n_rows = n_rows;
+  a.head_bytes = kv->head_dim * a.esz;
+  a.lens_out = lens_out;
+  a.seen_out = seen_out;
+  a.weights = weights;
+  a.pos = pos;
+  const cudaError_t ce = launch_k(1, k_paged_append, dim3(n_rows + 1), dim3(PP_THREADS), 0, (cudaStream_t)cuda_stream, a);
+  if (ce != cudaSuccess) return e.fail(LSP_ERR_CUDA, "%s: launch failed (%s)", who, cudaGetErrorString(ce));
+  return LSP_OK;
+}
+
+size_t lsp_paged_attention_workspace(const lsp_paged_kv* kv, int n_heads, int n_rows, int with_weights) {
+  PagedView pv;
+  if (check_view(Err{nullptr, 0}, "", kv, &pv) != LSP_OK || n_heads < 1 || n_rows < 0) return 0;
+  return attn_layout(kv, n_heads, n_rows, with_weights).total;
+}
+
+int lsp_paged_attention(const lsp_paged_kv* kv, const void* q, long long ldq, int n_heads, const int32_t* lens, const int32_t* row_off,
+                        int max_rows, int n_rows, float scale, void* out, long long ldo, float* lse, const float* weights_in,
+                        float* weights_out, void* workspace, size_t workspace_bytes, void* cuda_stream, char* err, size_t err_len) {
+  const Err e{err, err_len};
+  const char* who = "lsp_paged_attention";
+  PagedAttnArgs a;
+  int rc = check_view(e, who, kv, &a.pv);
+  if (rc) return rc;
+  rc = check_rows(e, who, kv, row_off, max_rows, n_rows);
+  if (rc) return rc;
+  if (!lens || !workspace || (n_rows > 0 && (!q || !out))) return e.fail(LSP_ERR_ARG, "%s: NULL pointer", who);
+  if (off_boundary(lens, row_off, lse, weights_in, weights_out)) return e.fail(LSP_ERR_ARG, "%s: misaligned array", who);
+  if (n_heads < 1 || n_heads % kv->n_kv_heads) return e.fail(LSP_ERR_SHAPE, "%s: %d query heads over %d KV heads", who, n_heads, kv->n_kv_heads);
+  if (!(scale > 0.f) || std::isinf(scale)) return e.fail(LSP_ERR_ARG, "%s: scale must be positive and finite", who);
+  if (weights_in && !weights_out) return e.fail(LSP_ERR_ARG, "%s: weights_in without weights_out", who);
+  const int esz = kv->dtype == 0 ? 4 : 2, qd = n_heads * kv->head_dim;
+  if ((ldq * esz) % 16 || (ldo * esz) % 16 || ((uintptr_t)q & 15) || ((uintptr_t)out & 15) || ldq < qd || ldo < qd)
+    return e.fail(LSP_ERR_ARG, "%s: rows of q and out must be 16-byte aligned and at least n_heads x head_dim elements apart", who);
+  if ((uintptr_t)workspace & 255) return e.fail(LSP_ERR_ARG, "%s: the workspace must be 256-byte aligned", who);
+  const AttnLayout L = attn_layout(kv, n_heads, n_rows, weights_out != nullptr);
+  if (workspace_bytes < L.total) return e.fail(LSP_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, L.total);
+  a.group = n_heads / kv->n_kv_heads;
+  const long long rows_unit = (long long)max_rows * a.group, tiles = (rows_unit + PA_ROWS - 1) / PA_ROWS;
+  const long long cap = (long long)kv->max_pages * kv->page_size, units = tiles * kv->batch * kv->n_kv_heads;
+  if (units * PA_ROWS + (long long)kv->batch * kv->n_kv_heads * (cap / PJ_KEYS + 1) > 0x7fffffffll || units * (cap / PA_CHUNK + 1) > 0x7fffffffll)
+    return e.fail(LSP_ERR_SHAPE, "%s: batch x heads x rows x slots too large for one call", who);
+  if (weights_out && rows_unit > 8192) return e.fail(LSP_ERR_SHAPE, "%s: weights of more than 8192 (row, head) pairs per KV head", who);
+  if (n_rows == 0 && !weights_out) return LSP_OK;
+  char* ws = (char*)workspace;
+  a.q = q;
+  a.out = out;
+  a.ldq = ldq;
+  a.ldo = ldo;
+  a.lens = lens;
+  a.row_off = row_off;
+  a.hq = n_heads;
+  a.max_rows = max_rows;
+  a.n_rows = n_rows;
+  a.n_cta = 0;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.lse = lse;
+  a.part_o = (float*)(ws + L.part_o);
+  a.part_ml = (float2*)(ws + L.part_ml);
+  a.row_ml = (float2*)(ws + L.row_ml);
+  a.scores = weights_out ? (float*)(ws + L.scores) : nullptr;
+  a.weights_in = weights_in;
+  a.weights_out = weights_out;
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  cudaError_t ce;
+  if (kv->dtype == 1)
+    ce = kv->head_dim == 128 ? launch_attention<bf16, 128>(a, (int)tiles, st) : launch_attention<bf16, 64>(a, (int)tiles, st);
+  else
+    ce = kv->head_dim == 128 ? launch_attention<float, 128>(a, (int)tiles, st) : launch_attention<float, 64>(a, (int)tiles, st);
+  if (ce != cudaSuccess) return e.fail(LSP_ERR_CUDA, "%s: launch failed (%s)", who, cudaGetErrorString(ce));
+  return LSP_OK;
+}
+
+size_t lsp_paged_evict_workspace(const lsp_paged_kv* kv, int budget) {
+  PagedView pv;
+  if (check_view(Err{nullptr, 0}, "", kv, &pv) != LSP_OK || budget < 1) return 0;
+  return align256((size_t)kv->batch * kv->n_kv_heads * (1 + 2 * (size_t)evict_moves(kv, budget)) * 4);
+}
+
+int lsp_paged_evict(const lsp_paged_kv* kv, const float* weights, const int32_t* pos, const int32_t* lens, const int32_t* seen, int budget,
+                    int n_sink, int n_recent, float* weights_out, int32_t* pos_out, int32_t* lens_out, void* workspace,
+                    size_t workspace_bytes, void* cuda_stream, char* err, size_t err_len) {
+  const Err e{err, err_len};
+  const char* who = "lsp_paged_evict";
+  PagedEvictArgs a;
+  int rc = check_view(e, who, kv, &a.pv);
+  if (rc) return rc;
+  if (!weights || !lens || !weights_out || !lens_out || !workspace) return e.fail(LSP_ERR_ARG, "%s: NULL pointer", who);
+  if (off_boundary(weights, pos, lens, seen, weights_out, pos_out, lens_out)) return e.fail(LSP_ERR_ARG, "%s: misaligned array", who);
+  if (pos && !pos_out) return e.fail(LSP_ERR_ARG, "%s: pos without pos_out", who);
+  if (budget < 1 || n_sink < 0 || n_recent < 0 || (long long)n_sink + n_recent > budget)
+    return e.fail(LSP_ERR_ARG, "%s: budget %d must be positive and hold n_sink %d + n_recent %d", who, budget, n_sink, n_recent);
+  const long long cap = (long long)kv->max_pages * kv->page_size;
+  const size_t nb = (size_t)kv->batch * 4, nw = (size_t)kv->batch * kv->n_kv_heads * cap * 4;
+  if (overlap(lens, lens_out, nb, nb) || overlap(seen, lens_out, nb, nb) || overlap(weights, weights_out, nw, nw) || overlap(pos, pos_out, nw, nw) ||
+      overlap(weights, pos_out, nw, nw) || overlap(pos, weights_out, nw, nw) || overlap(weights_out, pos_out, nw, nw))
+    return e.fail(LSP_ERR_ARG, "%s: outputs must not overlap what the call reads, nor one another", who);
+  if ((uintptr_t)workspace & 255) return e.fail(LSP_ERR_ARG, "%s: the workspace must be 256-byte aligned", who);
+  const size_t need = lsp_paged_evict_workspace(kv, budget);
+  if (workspace_bytes < need) return e.fail(LSP_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, need);
+  a.weights = weights;
+  a.pos = pos;
+  a.lens = lens;
+  a.seen = seen;
+  a.budget = budget;
+  a.n_sink = n_sink;
+  a.n_recent = n_recent;
+  a.max_moves = (int)evict_moves(kv, budget);
+  a.weights_out = weights_out;
+  a.pos_out = pos_out;
+  a.lens_out = lens_out;
+  a.moves = (int*)workspace;
+  a.esz = kv->dtype == 0 ? 4 : 2;
+  a.head_bytes = kv->head_dim * a.esz;
+  const cudaStream_t st = (cudaStream_t)cuda_stream;
+  const int units = kv->batch * kv->n_kv_heads;
+  const size_t smem = (size_t)PE_BINS * 4 + (size_t)(cap + 31) / 32 * 4;
+  cudaError_t ce = cudaFuncSetAttribute(k_paged_select, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (ce == cudaSuccess) ce = launch_k(1, k_paged_select, dim3(units), dim3(PE_THREADS), smem, st, a);
+  if (ce == cudaSuccess && a.max_moves > 0)
+    ce = launch_k(1, k_paged_move, dim3(units, (a.max_moves + PM_WARPS * PM_PAIRS - 1) / (PM_WARPS * PM_PAIRS)), dim3(PM_WARPS * 32), 0, st, a);
+  if (ce != cudaSuccess) return e.fail(LSP_ERR_CUDA, "%s: launch failed (%s)", who, cudaGetErrorString(ce));
+  return LSP_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,55 @@
+// What the kernels of the paged key-value cache share: its description, lookups with their checks, how the work of an
+// attention is dealt.
+#pragma once
+#include "common.cuh"
+
+namespace lsp {
+
+// bits of the status word (lsp_paged_kv.status)
+constexpr int PG_BAD_LEN = 1, PG_BAD_PAGE = 2, PG_BAD_ROWS = 4;
+
+struct PagedView {
+  char *k, *v;                                  // pools (element type T of the kernel)
+  const int* table;                             // [batch][max_pages], or null: page p of sequence b is b * max_pages + p
+  int* status;
+  long long page_stride, row_stride, head_stride;      // elements
+  int n_pages, page, max_pages, batch, hkv;
+};
+
+__device__ __forceinline__ void pg_flag(const PagedView& pv, int bit) {
+  if (pv.status) atomicOr(pv.status, bit);
+}
+__device__ __forceinline__ int pg_capacity(const PagedView& pv) { return pv.max_pages * pv.page; }
+
+// Slots in use of sequence b, inside [0, capacity].
+__device__ __forceinline__ int pg_len(const PagedView& pv, const int* lens, int b) {
+  const int n = lens[b], cap = pg_capacity(pv);
+  if (n < 0 || n > cap) {
+    pg_flag(pv, PG_BAD_LEN);
+    return n < 0 ? 0 : cap;
+  }
+  return n;
+}
+// Id of the page that holds slot j of sequence b (0 <= j < capacity); -1 with the flag set where the table names no page of the pool.
+__device__ __forceinline__ int pg_page(const PagedView& pv, int b, int j) {
+  const int p = j / pv.page;
+  const int id = pv.table ? pv.table[(long long)b * pv.max_pages + p] : b * pv.max_pages + p;
+  if (id < 0 || id >= pv.n_pages) {
+    pg_flag(pv, PG_BAD_PAGE);
+    return -1;
+  }
+  return id;
+}
+// Packed rows of sequence b: first one and count (0 with the flag set where the offsets leave the caller's rows).
+struct RowSpan { int first, n; };
+__device__ __forceinline__ RowSpan pg_rows(const PagedView& pv, const int* row_off, int b, int max_rows, int n_rows) {
+  if (!row_off) return RowSpan{b * max_rows, max_rows};
+  const int r0 = row_off[b], r1 = row_off[b + 1];
+  if (r0 < 0 || r1 < r0 || r1 > n_rows || r1 - r0 > max_rows) {
+    pg_flag(pv, PG_BAD_ROWS);
+    return RowSpan{0, 0};
+  }
+  return RowSpan{r0, r1 - r0};
+}
+
+}  // namespace lsp
