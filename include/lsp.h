@@ -309,8 +309,9 @@ int lsp_paged_append(const lsp_paged_kv* kv, const void* k_new, const void* v_ne
  * elements apart.  The slots are split over the device and the parts joined in a fixed order: the same inputs give the same bits.
  * Accumulation in fp32; bf16 softmax weights enter the product with V as a sum of two.  Meant for up to some dozens of (row, head)
  * pairs per KV head; a tile of 16 of them reads the cache once.
- * workspace: device, 256-byte aligned, lsp_paged_attention_workspace() bytes (for weights it holds the scores), uninitialised; calls that share
- * one must not overlap on the device. */
+ * workspace: device, 256-byte aligned, lsp_paged_attention_workspace() bytes (for weights it holds the scores).  Its first 4096 bytes hold
+ * counters: the caller clears them once, every call leaves them clear; the rest may hold anything.  Calls that share a workspace must not overlap
+ * on the device. */
 size_t lsp_paged_attention_workspace(const lsp_paged_kv* kv, int n_heads, int n_rows, int with_weights);
 int lsp_paged_attention(const lsp_paged_kv* kv, const void* q, long long ldq, int n_heads, const int32_t* lens,
                         const int32_t* row_off, int max_rows, int n_rows, float scale, void* out, long long ldo, float* lse,
@@ -326,7 +327,7 @@ int lsp_paged_attention(const lsp_paged_kv* kv, const void* q, long long ldq, in
  *   lens, seen          device [batch]; seen NULL: lens
  *   weights_out, pos_out, lens_out   as the inputs, not overlapping them; lens_out = min(lens, budget); slots behind it are not written
  * Pages behind ceil(lens_out / page_size) are free afterwards.  The pages of a sequence that is thinned must belong to it alone.
- * workspace: as above, lsp_paged_evict_workspace() bytes. */
+ * workspace: lsp_paged_evict_workspace() bytes, aligned as above; the attention's may be taken (its counters are left alone). */
 size_t lsp_paged_evict_workspace(const lsp_paged_kv* kv, int budget);
 int lsp_paged_evict(const lsp_paged_kv* kv, const float* weights, const int32_t* pos, const int32_t* lens, const int32_t* seen,
                     int budget, int n_sink, int n_recent, float* weights_out, int32_t* pos_out, int32_t* lens_out,

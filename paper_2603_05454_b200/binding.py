@@ -386,20 +386,23 @@ class PagedKVCache:
         if k_pool.shape[3] > 1 and k_pool.stride(3) != 1:
             raise ValueError("the elements of a head must be contiguous")
         n_pages, page_size, n_kv, dh = k_pool.shape
+        self.device, self.dtype, self._index = k_pool.device, k_pool.dtype, k_pool.get_device()
         if page_table is not None:
             if page_table.dim() != 2:
                 raise ValueError("page_table must be [batch, max_pages]")
-            self._tensor("page_table", page_table, torch.int32, tuple(page_table.shape), k_pool.device)
+            self._tensor("page_table", page_table, torch.int32, page_table.shape)
             self.batch, self.max_pages = page_table.shape
             if batch not in (None, self.batch):
                 raise ValueError(f"page_table has {self.batch} sequences, not {batch}")
         else:
             self.batch = batch or 1
             self.max_pages = n_pages // self.batch
-        self.device, self.dtype = k_pool.device, k_pool.dtype
         self.n_heads, self.n_kv_heads, self.head_dim = n_heads, n_kv, dh
         self.max_rows = max_rows
         self.capacity = self.max_pages * page_size
+        self._per_seq, self._per_slot = torch.Size((self.batch,)), torch.Size((self.batch, n_kv, self.capacity))
+        self._offsets = torch.Size((self.batch + 1,))
+        self._q_width, self._kv_width, self._scale = n_heads * dh, n_kv * dh, dh ** -0.5
         self.k_pool, self.v_pool, self.page_table = k_pool, v_pool, page_table
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._kv = PagedKV(k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr() if page_table is not None else None,
@@ -415,26 +418,29 @@ class PagedKVCache:
         # (an eviction moves most where half of the slots go)
         need = max(need, lib.lsp_paged_evict_workspace(self._ref, max(1, self.capacity // 2)))
         self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+        self.workspace[:4096].zero_()          # arrival counters
+        self._ws, self._ws_bytes = self.workspace.data_ptr(), need
 
-    @staticmethod
-    def _tensor(name, t, dtype, shape, device):
-        if t.dtype != dtype or tuple(t.shape) != shape or t.device != device or not t.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {list(shape)} on {device}")
+    # (the checks run with every call of a few microseconds: each is one comparison of what torch hands out as it is)
+    def _tensor(self, name, t, dtype, shape):
+        """Address of a contiguous tensor; None for None."""
+        if t is None:
+            return None
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != self._index or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {list(shape)} on {self.device}")
         return t.data_ptr()
 
-    def _opt(self, name, t, dtype, shape):
-        return None if t is None else self._tensor(name, t, dtype, shape, self.device)
-
     def _rows(self, name, t, width):
-        """Packed rows [n_rows, width], rows any distance apart."""
-        if t.dtype != self.dtype or t.dim() != 2 or t.shape[1] != width or t.device != self.device or (width > 1 and t.stride(1) != 1):
+        """Address, count and distance of packed rows [n_rows, width]."""
+        if t.dtype is not self.dtype or t.dim() != 2 or t.shape[1] != width or t.get_device() != self._index or t.stride(1) != 1:
             raise ValueError(f"{name} must be a {self.dtype} tensor of shape [rows, {width}] on {self.device}, elements of a row contiguous")
-        return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), width))
+        n = t.shape[0]
+        return t.data_ptr(), n, t.stride(0) if n > 1 else max(t.stride(0), width)
 
     def _row_off(self, row_off, n_rows, max_rows):
-        """Pointer to the offsets and the bound of a sequence's rows."""
+        """Address of the offsets and the bound of a sequence's rows."""
         if row_off is not None:
-            return self._tensor("row_off", row_off, torch.int32, (self.batch + 1,), self.device), max_rows or self.max_rows
+            return self._tensor("row_off", row_off, torch.int32, self._offsets), max_rows or self.max_rows
         if n_rows % self.batch or n_rows == 0:
             raise ValueError(f"without row_off every one of the {self.batch} sequences has as many rows: {n_rows} rows do not divide")
         return None, n_rows // self.batch
@@ -444,56 +450,51 @@ class PagedKVCache:
             raise LSPError(rc, self._err.value.decode())
 
     def _call(self, stream, fn, *args):
-        sptr = torch.cuda.current_stream(self.device).cuda_stream if stream is None else stream.cuda_stream
-        if torch.cuda.current_device() == self.device.index:
+        sptr = torch._C._cuda_getCurrentRawStream(self._index) if stream is None else stream.cuda_stream
+        if torch._C._cuda_getDevice() == self._index:
             rc = fn(self._ref, *args, sptr, self._err, 256)
         else:
             with torch.cuda.device(self.device):
                 rc = fn(self._ref, *args, sptr, self._err, 256)
-        self._check(rc)
+        if rc != 0:
+            self._check(rc)
 
     def append(self, k_new: torch.Tensor, v_new: torch.Tensor, lens: torch.Tensor, lens_out: torch.Tensor, *, row_off=None,
                max_rows: Optional[int] = None, weights=None, pos=None, seen=None, seen_out=None, stream=None):
         """Writes packed rows k_new, v_new [n_rows, n_kv_heads * head_dim] behind the lens[b] cached ones (lsp_paged_append)."""
-        width = self.n_kv_heads * self.head_dim
-        kp, ld = self._rows("k_new", k_new, width)
-        vp, ldv = self._rows("v_new", v_new, width)
-        if v_new.shape != k_new.shape or ldv != ld:
+        kp, n, ld = self._rows("k_new", k_new, self._kv_width)
+        vp, nv, ldv = self._rows("v_new", v_new, self._kv_width)
+        if nv != n or ldv != ld:
             raise ValueError("k_new and v_new need one shape and one row stride")
-        n = k_new.shape[0]
         off, most = self._row_off(row_off, n, max_rows)
-        b, per_slot = (self.batch,), (self.batch, self.n_kv_heads, self.capacity)
-        self._call(stream, lib.lsp_paged_append, kp, vp, ld, self._opt("lens", lens, torch.int32, b), off, most, n,
-                   self._opt("lens_out", lens_out, torch.int32, b), self._opt("weights", weights, torch.float32, per_slot),
-                   self._opt("pos", pos, torch.int32, per_slot), self._opt("seen", seen, torch.int32, b),
-                   self._opt("seen_out", seen_out, torch.int32, b))
+        i32, b, tensor = torch.int32, self._per_seq, self._tensor
+        self._call(stream, lib.lsp_paged_append, kp, vp, ld, tensor("lens", lens, i32, b), off, most, n, tensor("lens_out", lens_out, i32, b),
+                   tensor("weights", weights, torch.float32, self._per_slot), tensor("pos", pos, i32, self._per_slot), tensor("seen", seen, i32, b),
+                   tensor("seen_out", seen_out, i32, b))
         return lens_out
 
     def attention(self, q: torch.Tensor, lens: torch.Tensor, out: torch.Tensor, *, row_off=None, max_rows: Optional[int] = None,
                   scale: Optional[float] = None, lse=None, weights_in=None, weights_out=None, stream=None):
         """Attention of packed rows q [n_rows, n_heads * head_dim] over their sequences' slots (lsp_paged_attention); scale: 1 / sqrt(head_dim)."""
-        width = self.n_heads * self.head_dim
-        qp, ldq = self._rows("q", q, width)
-        op, ldo = self._rows("out", out, width)
-        n = q.shape[0]
-        if out.shape[0] != n:
-            raise ValueError(f"q has {n} rows, out {out.shape[0]}")
+        qp, n, ldq = self._rows("q", q, self._q_width)
+        op, no, ldo = self._rows("out", out, self._q_width)
+        if no != n:
+            raise ValueError(f"q has {n} rows, out {no}")
         off, most = self._row_off(row_off, n, max_rows)
-        per_slot = (self.batch, self.n_kv_heads, self.capacity)
-        self._call(stream, lib.lsp_paged_attention, qp, ldq, self.n_heads, self._opt("lens", lens, torch.int32, (self.batch,)), off, most, n,
-                   self.head_dim ** -0.5 if scale is None else scale, op, ldo, self._opt("lse", lse, torch.float32, (n, self.n_heads)),
-                   self._opt("weights_in", weights_in, torch.float32, per_slot), self._opt("weights_out", weights_out, torch.float32, per_slot),
-                   self.workspace.data_ptr(), self.workspace.numel())
+        f32, tensor = torch.float32, self._tensor
+        self._call(stream, lib.lsp_paged_attention, qp, ldq, self.n_heads, tensor("lens", lens, torch.int32, self._per_seq), off, most, n,
+                   self._scale if scale is None else scale, op, ldo, None if lse is None else tensor("lse", lse, f32, (n, self.n_heads)),
+                   tensor("weights_in", weights_in, f32, self._per_slot), tensor("weights_out", weights_out, f32, self._per_slot),
+                   self._ws, self._ws_bytes)
         return out
 
     def evict(self, weights: torch.Tensor, lens: torch.Tensor, budget: int, weights_out: torch.Tensor, lens_out: torch.Tensor, *,
               n_sink: int = 0, n_recent: int = 0, pos=None, pos_out=None, seen=None, stream=None):
         """Thins every sequence to at most budget slots per KV head (lsp_paged_evict)."""
-        b, per_slot = (self.batch,), (self.batch, self.n_kv_heads, self.capacity)
-        self._call(stream, lib.lsp_paged_evict, self._opt("weights", weights, torch.float32, per_slot), self._opt("pos", pos, torch.int32, per_slot),
-                   self._opt("lens", lens, torch.int32, b), self._opt("seen", seen, torch.int32, b), budget, n_sink, n_recent,
-                   self._opt("weights_out", weights_out, torch.float32, per_slot), self._opt("pos_out", pos_out, torch.int32, per_slot),
-                   self._opt("lens_out", lens_out, torch.int32, b), self.workspace.data_ptr(), self.workspace.numel())
+        i32, f32, b, slots, tensor = torch.int32, torch.float32, self._per_seq, self._per_slot, self._tensor
+        self._call(stream, lib.lsp_paged_evict, tensor("weights", weights, f32, slots), tensor("pos", pos, i32, slots), tensor("lens", lens, i32, b),
+                   tensor("seen", seen, i32, b), budget, n_sink, n_recent, tensor("weights_out", weights_out, f32, slots),
+                   tensor("pos_out", pos_out, i32, slots), tensor("lens_out", lens_out, i32, b), self._ws, self._ws_bytes)
         return lens_out
 
     def check(self):

@@ -70,14 +70,17 @@ bool overlap(const void* a, const void* b, size_t bytes_a, size_t bytes_b) {
   return a && b && (const char*)a < (const char*)b + bytes_b && (const char*)b < (const char*)a + bytes_a;
 }
 
-struct AttnLayout { size_t part_o, part_ml, row_ml, scores, total; };
+constexpr size_t kCounters = 4096;        // the first bytes of a workspace: arrival counters, 0 between calls
+static_assert(PA_MAX_CTAS * 4 <= kCounters, "a counter per CTA");
+
+struct AttnLayout { size_t part_o, part_ml, row_lse, scores, total; };
 AttnLayout attn_layout(const lsp_paged_kv* kv, int n_heads, int n_rows, int with_weights) {
   AttnLayout L;
-  size_t at = 0;
+  size_t at = kCounters;
   auto take = [&](size_t bytes) { const size_t o = at; at += align256(bytes); return o; };
   L.part_o = take((size_t)2 * PA_MAX_CTAS * PA_ROWS * kv->head_dim * 4);
   L.part_ml = take((size_t)2 * PA_MAX_CTAS * PA_ROWS * 8);
-  L.row_ml = take(with_weights ? (size_t)n_rows * n_heads * 8 : 0);
+  L.row_lse = take(with_weights ? (size_t)n_rows * n_heads * 4 : 0);
   L.scores = take(with_weights ? (size_t)n_rows * n_heads * kv->max_pages * kv->page_size * 4 : 0);
   L.total = at;
   return L;
@@ -91,11 +94,28 @@ long long evict_moves(const lsp_paged_kv* kv, int budget) {
 template <typename T, int DH>
 cudaError_t launch_attention(const PagedAttnArgs& a0, int tiles, cudaStream_t stream) {
   PagedAttnArgs a = a0;
-  void (*kern)(PagedAttnArgs);
-  if constexpr (sizeof(T) == 2) kern = k_paged_attn_mma<DH>;
-  else kern = k_paged_attn_simt<DH>;
-  constexpr int smem = pa_smem_bytes<T, DH>();
-  constexpr int per_sm = 2 * (smem + 1024) <= 228 * 1024 ? 2 : 1;
+  using S = PaSmem<T, DH>;
+  void (*kern)(PagedAttnArgs) = nullptr;
+  a.q_rows = std::min(PA_ROWS, a.max_rows * a.group);
+  if constexpr (sizeof(T) == 2) {
+    kern = k_paged_attn_mma<DH>;
+  } else {
+    kern = a.q_rows == 1 ? k_paged_attn_simt<DH, 1> : a.q_rows == 2 ? k_paged_attn_simt<DH, 2> : a.q_rows <= 4 ? k_paged_attn_simt<DH, 4>
+         : a.q_rows <= 8 ? k_paged_attn_simt<DH, 8> : k_paged_attn_simt<DH, 16>;
+  }
+  // Two CTAs an SM where their shared memory allows it; as many rows added at a time as are left room for.
+  constexpr int kStatic = 128, kSm = 228 * 1024, kCta = 227 * 1024 - kStatic, kOwn = 1024 + kStatic;
+  constexpr int per_sm = 2 * (S::RINGS + kOwn) <= kSm ? 2 : 1;
+  int n_per_sm = 0, smem = 0;
+  for (int want = per_sm; want >= 1 && !n_per_sm; --want)
+    for (int rows = 4; rows >= 1 && !n_per_sm; rows /= 2) {
+      smem = S::total(a.q_rows, rows, a.pv.batch);
+      if (smem <= kCta && want * (smem + kOwn) <= kSm) {
+        a.merge_rows = rows;
+        n_per_sm = want;
+      }
+    }
+  if (!n_per_sm) return cudaErrorInvalidConfiguration;
   int dev = 0, n_sm = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev);
@@ -103,15 +123,12 @@ cudaError_t launch_attention(const PagedAttnArgs& a0, int tiles, cudaStream_t st
   if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   const long long cap = (long long)a.pv.max_pages * a.pv.page;
-  const long long most = (cap + PA_CHUNK - 1) / PA_CHUNK * a.pv.batch * a.pv.hkv * tiles;       // chunks, if every sequence were full
-  a.n_cta = (int)std::min<long long>(most, std::min(per_sm * n_sm, PA_MAX_CTAS));
-  e = launch_k(1, kern, dim3(a.n_cta), dim3(PA_WARPS * 32), (size_t)smem, stream, a);
-  if (e != cudaSuccess) return e;
-  const int rows_tile = std::min(PA_ROWS, a.max_rows * a.group);
-  const int join_blocks = a.pv.batch * a.pv.hkv * tiles * rows_tile;
-  const int key_blocks = a.scores ? (int)((cap + PJ_KEYS - 1) / PJ_KEYS) : 0;
-  return launch_k(1, k_paged_join<T, DH>, dim3(join_blocks + a.pv.batch * a.pv.hkv * key_blocks), dim3(PJ_THREADS),
-                  a.scores ? (size_t)a.max_rows * a.group * 4 : 0, stream, a, tiles, rows_tile, join_blocks, key_blocks);
+  const long long most = ((cap + PA_CHUNK - 1) / PA_CHUNK + PA_UNIT_COST) * a.pv.batch * a.pv.hkv * tiles;       // numbers to deal, if every sequence were full
+  a.n_cta = (int)std::min<long long>(most, std::min(n_per_sm * n_sm, PA_MAX_CTAS));
+  e = launch_k(1, kern, dim3(a.n_cta), dim3(PA_THREADS), (size_t)smem, stream, a);
+  if (e != cudaSuccess || !a.scores) return e;
+  const int key_blocks = (int)((cap + PW_KEYS - 1) / PW_KEYS);
+  return launch_k(1, k_paged_weights, dim3(a.pv.batch * a.pv.hkv * key_blocks), dim3(PW_THREADS), (size_t)a.max_rows * a.group * 4, stream, a, key_blocks);
 }
 
 }  // namespace
@@ -186,7 +203,7 @@ int lsp_paged_attention(const lsp_paged_kv* kv, const void* q, long long ldq, in
   a.group = n_heads / kv->n_kv_heads;
   const long long rows_unit = (long long)max_rows * a.group, tiles = (rows_unit + PA_ROWS - 1) / PA_ROWS;
   const long long cap = (long long)kv->max_pages * kv->page_size, units = tiles * kv->batch * kv->n_kv_heads;
-  if (units * PA_ROWS + (long long)kv->batch * kv->n_kv_heads * (cap / PJ_KEYS + 1) > 0x7fffffffll || units * (cap / PA_CHUNK + 1) > 0x7fffffffll)
+  if ((long long)kv->batch * kv->n_kv_heads * (cap / PW_KEYS + 1) > 0x7fffffffll || units * (cap / PA_CHUNK + 1 + PA_UNIT_COST) > 0x7fffffffll)
     return e.fail(LSP_ERR_SHAPE, "%s: batch x heads x rows x slots too large for one call", who);
   if (weights_out && rows_unit > 8192) return e.fail(LSP_ERR_SHAPE, "%s: weights of more than 8192 (row, head) pairs per KV head", who);
   if (n_rows == 0 && !weights_out) return LSP_OK;
@@ -205,7 +222,8 @@ int lsp_paged_attention(const lsp_paged_kv* kv, const void* q, long long ldq, in
   a.lse = lse;
   a.part_o = (float*)(ws + L.part_o);
   a.part_ml = (float2*)(ws + L.part_ml);
-  a.row_ml = (float2*)(ws + L.row_ml);
+  a.arrived = (unsigned*)ws;
+  a.row_lse = (float*)(ws + L.row_lse);
   a.scores = weights_out ? (float*)(ws + L.scores) : nullptr;
   a.weights_in = weights_in;
   a.weights_out = weights_out;
@@ -222,7 +240,7 @@ int lsp_paged_attention(const lsp_paged_kv* kv, const void* q, long long ldq, in
 size_t lsp_paged_evict_workspace(const lsp_paged_kv* kv, int budget) {
   PagedView pv;
   if (check_view(Err{nullptr, 0}, "", kv, &pv) != LSP_OK || budget < 1) return 0;
-  return align256((size_t)kv->batch * kv->n_kv_heads * (1 + 2 * (size_t)evict_moves(kv, budget)) * 4);
+  return kCounters + align256((size_t)kv->batch * kv->n_kv_heads * (1 + 2 * (size_t)evict_moves(kv, budget)) * 4);
 }
 
 int lsp_paged_evict(const lsp_paged_kv* kv, const float* weights, const int32_t* pos, const int32_t* lens, const int32_t* seen, int budget,
@@ -257,7 +275,7 @@ int lsp_paged_evict(const lsp_paged_kv* kv, const float* weights, const int32_t*
   a.weights_out = weights_out;
   a.pos_out = pos_out;
   a.lens_out = lens_out;
-  a.moves = (int*)workspace;
+  a.moves = (int*)((char*)workspace + kCounters);
   a.esz = kv->dtype == 0 ? 4 : 2;
   a.head_bytes = kv->head_dim * a.esz;
   const cudaStream_t st = (cudaStream_t)cuda_stream;

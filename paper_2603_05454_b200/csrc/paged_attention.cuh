@@ -6,12 +6,13 @@
 // Every row sees every slot (the library's attention is bidirectional).
 //
 // The stream of K and V from HBM bounds it: 4 dh rows * group flops per 4 dh bytes.  So:
-//  * The slots of every (sequence, KV head, tile of 16 (row, head) pairs) are cut into chunks of 64, all chunks of the batch are
-//    numbered through, and each CTA of a grid that fills the SMs takes an equal run of them, whatever the lengths are.  A unit
-//    that one CTA holds whole is written by it; the parts (m, l, o) of a unit that a run's end cuts go to the workspace and
-//    k_paged_join adds them in order.  No atomics, no counters, the same bits every time.
+//  * The slots of every unit, a (sequence, KV head, tile of 16 (row, head) pairs), are cut into chunks of 64; all chunks of the batch are
+//    numbered through, with room for what a unit costs besides, and each CTA of a grid that fills the SMs takes an equal run of the
+//    numbers, whatever the lengths are.  A unit that one CTA holds whole is written by it; the parts (m, l, o) of a unit that a run's
+//    end cuts go to the workspace, and the last of its CTAs to arrive adds them in their order: the same bits every time.
 //  * A warp takes 16 slots of a chunk and loads them itself: a ring of its own in shared memory, filled by cp.async, page ids one
-//    turn ahead of the rows they lead to.  The warps of a CTA meet only where a unit ends.
+//    turn ahead of the rows they lead to, the queries of the next unit with its first chunk.  The warps of a CTA meet only where a unit
+//    begins and ends.
 //  * mma.sync m16n8k16, not tcgen05: a tile has at most 16 rows (often one), an M of 128 would be 1/8 to 1/128 full, and the
 //    legacy pipe needs a third of the time that the bytes take.
 #pragma once
@@ -22,12 +23,13 @@ namespace lsp {
 
 constexpr int PA_CHUNK = 64;            // slots of a chunk: 16 per warp
 constexpr int PA_WARPS = 4;
-constexpr int PA_STAGES = 3;
+constexpr int PA_THREADS = PA_WARPS * 32;
 constexpr int PA_ROWS = 16;             // (row, head) pairs of a unit
 constexpr int PA_MAX_BATCH = 1024;
 constexpr int PA_MAX_CTAS = 512;
-constexpr int PJ_THREADS = 256;
-constexpr int PJ_KEYS = 1024;           // slots of a weights block
+constexpr int PA_UNIT_COST = 2;         // what a unit costs besides its chunks, in chunks (queries, adding the warps' parts)
+constexpr int PW_THREADS = 256;
+constexpr int PW_KEYS = 1024;           // slots of a weights block
 
 struct PagedAttnArgs {
   PagedView pv;
@@ -38,148 +40,123 @@ struct PagedAttnArgs {
   int hq, group, max_rows, n_rows, n_cta;
   float scale_log2;
   float* lse;                  // [n_rows][hq] or null
+  unsigned* arrived;           // [n_cta]: parts of the cut unit that begins in CTA i's run; 0 between calls
   float* part_o;               // [2 n_cta][16][dh]
   float2* part_ml;             // [2 n_cta][16]: m (in log2 units), l
   float* scores;               // [n_rows][hq][capacity] in log2 units, or null: no weights wanted
-  float2* row_ml;              // [n_rows][hq]: m, l of units that one CTA held whole (with weights)
+  float* row_lse;              // [n_rows][hq]: log2 of the sum of exponentials (with weights)
   const float* weights_in;
   float* weights_out;
+  int q_rows, merge_rows;      // rows of a query tile in shared memory; rows that the warps' parts are added for at a time
 };
 
+// Shared memory: queries (tiles in turn, a unit each), rings, parts of the warps, their (m, l), chunks before each sequence.
 template <typename T, int DH>
-constexpr int pa_stage_bytes() { return 2 * 16 * DH * (int)sizeof(T); }
-template <typename T, int DH>
-constexpr int pa_merge_bytes() { return 2 * 8 * DH * 4; }
-template <typename T, int DH>
-constexpr int pa_smem_bytes() {
-  return PA_WARPS * PA_STAGES * pa_stage_bytes<T, DH>() + pa_merge_bytes<T, DH>() + PA_WARPS * PA_ROWS * 8 + (PA_MAX_BATCH + 1) * 4 +
-         (sizeof(T) == 4 ? PA_ROWS * (DH + 4) * 4 : 0);
-}
+struct PaSmem {
+  static constexpr int STAGE = 2 * 16 * DH * (int)sizeof(T);          // 16 rows of K, 16 of V
+  static constexpr int STAGES = STAGE > 8192 && DH == 128 ? 2 : 3;    // (fp32 rows of 512 bytes: 64 KB in flight with two)
+  // Tiles of queries: those of as many units as chunks are asked for ahead, the next one's, and where the queries are not copied to registers at
+  // once the present one's (a warp may still be in it when another has reached the next).
+  static constexpr int Q_TILES = sizeof(T) == 4 ? STAGES + 1 : STAGES;
+  static constexpr int Q_ROW = DH * (int)sizeof(T) + (sizeof(T) == 4 ? 16 : 0);
+  static constexpr int RINGS = PA_WARPS * STAGES * STAGE;
+  __host__ __device__ static int q_tile(int q_rows) { return q_rows * Q_ROW; }
+  __host__ __device__ static int rings(int q_rows) { return (Q_TILES * q_tile(q_rows) + 127) / 128 * 128; }
+  __host__ __device__ static int merge(int q_rows) { return rings(q_rows) + RINGS; }
+  __host__ __device__ static int ml(int q_rows, int merge_rows) { return merge(q_rows) + PA_WARPS * merge_rows * DH * 4; }
+  __host__ __device__ static int pre(int q_rows, int merge_rows) { return ml(q_rows, merge_rows) + PA_WARPS * 4 * 8; }
+  __host__ __device__ static int total(int q_rows, int merge_rows, int batch) { return pre(q_rows, merge_rows) + (batch + 1) * 4; }
+};
 
-// Chunks of the units of sequence b, all KV heads and row tiles together, before b in pre[]; chunks of one unit: pa_chunks.
 __device__ __forceinline__ int pa_chunks(int len) { return (len + PA_CHUNK - 1) / PA_CHUNK; }
 
-// pre[b] = chunks of all sequences before b, b <= batch (a block-wide scan; ends with a barrier).
-template <int THREADS>
-__device__ __forceinline__ void pa_prefix(const PagedAttnArgs& a, int* pre, int* warp_sums) {
-  const int B = a.pv.batch, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  int carry = 0;
-  for (int b0 = 0; b0 < B; b0 += THREADS) {
-    const int b = b0 + threadIdx.x;
-    int n = 0;
-    if (b < B) {
-      const RowSpan rs = pg_rows(a.pv, a.row_off, b, a.max_rows, a.n_rows);
-      n = pa_chunks(pg_len(a.pv, a.lens, b)) * a.pv.hkv * ((rs.n * a.group + PA_ROWS - 1) / PA_ROWS);
-    }
-    int x = n;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
-    }
-    if (lane == 31) warp_sums[w] = x;
-    __syncthreads();
-    int before = carry, all = carry;
-#pragma unroll
-    for (int i = 0; i < THREADS / 32; ++i) {
-      const int s = warp_sums[i];
-      before += i < w ? s : 0;
-      all += s;
-    }
-    if (b < B) pre[b] = before + x - n;
-    carry = all;
+// pre[b] = numbers of all sequences before b, b <= batch.  Up to 32 sequences every warp computes and stores all of it (the same values) and waits
+// for no other; with more the block reads the lengths, all under way at once, and the first warp adds them up.
+__device__ __forceinline__ void pa_prefix(const PagedAttnArgs& a, int* pre) {
+  const int B = a.pv.batch, lane = threadIdx.x & 31;
+  if (B > 32) {
+    for (int b = threadIdx.x; b < B; b += PA_THREADS) pre[b] = a.lens[b];
     __syncthreads();
   }
-  if (threadIdx.x == 0) pre[B] = carry;
-  __syncthreads();
+  if (B <= 32 || threadIdx.x < 32) {
+    int carry = 0;
+#pragma unroll 1
+    for (int b0 = 0; b0 < B; b0 += 32) {
+      const int b = b0 + lane;
+      int n = 0;
+      if (b < B) {
+        const RowSpan rs = pg_rows(a.pv, a.row_off, b, a.max_rows, a.n_rows);
+        const int chunks = pa_chunks(pg_len(a.pv, B > 32 ? pre[b] : a.lens[b]));
+        n = chunks == 0 ? 0 : (chunks + PA_UNIT_COST) * a.pv.hkv * ((rs.n * a.group + PA_ROWS - 1) / PA_ROWS);
+      }
+      int x = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+      }
+      if (b < B) pre[b] = carry + x - n;
+      carry += __shfl_sync(0xffffffffu, x, 31);
+    }
+    if (lane == 0) pre[B] = carry;
+  }
+  if (B > 32) __syncthreads();
+  else __syncwarp();
 }
-// CTAs that get a run (at least a chunk each); first chunk of CTA i's run.
-__device__ __forceinline__ int pa_ctas(int total, int n_cta) { return min(total, n_cta); }
-__device__ __forceinline__ int pa_run(int total, int i, int n_cta) { return (int)((long long)total * i / n_cta); }
-// The CTA whose run holds chunk c.
-__device__ __forceinline__ int pa_owner(int total, int c, int n_cta) { return (int)((((long long)c + 1) * n_cta - 1) / total); }
+
+// How the numbers are dealt: CTA i of n (those that get at least one) has numbers [run(i), run(i + 1)), run(i) = floor(total i / n).
+struct PaDeal {
+  int total, n, q, r;
+  __device__ __forceinline__ PaDeal(int total_, int n_cta) : total(total_), n(min(total_, n_cta)), q(0), r(0) {
+    if (n > 0) {
+      q = total / n;
+      r = total - q * n;
+    }
+  }
+  __device__ __forceinline__ int run(int i) const { return i * q + i * r / n; }
+  // the CTA whose run holds number c (the estimate is off by one at most: 2^-24 of at most PA_MAX_CTAS, and the runs' rounding)
+  __device__ __forceinline__ int owner(int c) const {
+    int i = min(n - 1, (int)((float)c / (float)total * (float)n));
+    while (run(i) > c) --i;
+    while (run(i + 1) <= c) ++i;
+    return i;
+  }
+};
 
 // A place in the run: sequence, KV head, row tile, chunk of the unit.
 struct PaPlace {
-  int b, kvh, rt, chunk, chunks, len, left;        // left: chunks of this unit that belong to the run, from here on
+  int b, kvh, rt, chunk, chunks, len;
+  int u0, left;                 // the number of the unit's first chunk; chunks of the unit that belong to the run, from here on
+  __device__ __forceinline__ int next() const { return u0 + chunks + PA_UNIT_COST; }      // the following unit
 };
+// The place of the first chunk at or behind number c (some numbers are no chunks); left = 0 where the run holds none.
 __device__ __forceinline__ PaPlace pa_place(const PagedAttnArgs& a, const int* pre, int c, int hi) {
   PaPlace p;
-  int lo = 0, up = a.pv.batch;                     // pre[lo] <= c < pre[up]
-  while (up - lo > 1) {
-    const int mid = (lo + up) >> 1;
-    if (pre[mid] <= c) lo = mid; else up = mid;
+  p.left = 0;
+  while (c < hi) {
+    int lo = 0, up = a.pv.batch;                   // pre[lo] <= c < pre[up]
+    while (up - lo > 1) {
+      const int mid = (lo + up) >> 1;
+      if (pre[mid] <= c) lo = mid; else up = mid;
+    }
+    p.b = lo;
+    const int n = a.lens[lo], cap = pg_capacity(a.pv);
+    p.len = n > cap ? cap : n;
+    p.chunks = pa_chunks(p.len);
+    const int span = p.chunks + PA_UNIT_COST, tiles = (pre[lo + 1] - pre[lo]) / (span * a.pv.hkv);
+    const int u = (c - pre[lo]) / span;
+    p.u0 = pre[lo] + u * span;
+    p.chunk = c - p.u0;
+    p.kvh = u / tiles;
+    p.rt = u - p.kvh * tiles;
+    if (p.chunk < p.chunks) {
+      p.left = min(p.chunks - p.chunk, hi - c);
+      break;
+    }
+    c = p.next();
   }
-  p.b = lo;
-  const int n = a.lens[lo], cap = pg_capacity(a.pv);
-  p.len = n > cap ? cap : n;
-  p.chunks = pa_chunks(p.len);
-  const int tiles = (pre[lo + 1] - pre[lo]) / (p.chunks * a.pv.hkv);
-  const int u = (c - pre[lo]) / p.chunks;
-  p.chunk = c - pre[lo] - u * p.chunks;
-  p.kvh = u / tiles;
-  p.rt = u - p.kvh * tiles;
-  p.left = min(p.chunks - p.chunk, hi - c);
   return p;
 }
-
-// Byte offset of 16-byte chunk c of row r in a [16][DH] tile: chunks are exchanged within groups of eight by the row, so that eight
-// rows' chunks c lie in different banks.
-template <typename T, int DH>
-__device__ __forceinline__ int pa_at(int r, int c) {
-  return r * DH * (int)sizeof(T) + ((c ^ (r & 7)) << 4);
-}
-
-// One warp's loads: the rows of its 16 slots of a chunk, K then V, into one stage of its ring.
-template <typename T, int DH>
-struct PaLoader {
-  static constexpr int CPR = DH * (int)sizeof(T) / 16;      // 16-byte chunks of a row
-  const PagedAttnArgs& a;
-  const int* pre;
-  int c, hi, w, lane;
-  PaPlace p;
-  int page_id;                  // (lanes 0 to 15) page of this lane's slot of chunk c, asked for a turn ahead
-  __device__ __forceinline__ PaLoader(const PagedAttnArgs& a_, const int* pre_, int lo, int hi_, int w_, int lane_)
-      : a(a_), pre(pre_), c(lo), hi(hi_), w(w_), lane(lane_), page_id(-1) {
-    if (c < hi) {
-      p = pa_place(a, pre, c, hi);
-      ask();
-    }
-  }
-  __device__ __forceinline__ int slot() const { return p.chunk * PA_CHUNK + w * 16 + (lane & 15); }
-  __device__ __forceinline__ void ask() {
-    const int j = slot();
-    page_id = j < p.len ? pg_page(a.pv, p.b, j) : -1;
-  }
-  // Returns a mask of the rows that are real slots.
-  __device__ __forceinline__ unsigned issue(char* stage) {
-    unsigned live = 0;
-    if (c < hi) {
-      const int j = slot();
-      const bool ok = page_id >= 0;
-      live = __ballot_sync(0xffffffffu, ok) & 0xffffu;
-      const long long off = ok ? ((long long)page_id * a.pv.page_stride + (long long)(j % a.pv.page) * a.pv.row_stride + (long long)p.kvh * a.pv.head_stride) : 0;
-      const uint32_t ks = smem_u32(stage), vs = ks + 16 * DH * (int)sizeof(T);
-#pragma unroll
-      for (int i = 0; i < 16 * CPR / 32; ++i) {
-        const int r = (i * 32 + lane) / CPR, ch = (i * 32 + lane) % CPR;
-        const long long o = __shfl_sync(0xffffffffu, off, r) * (int)sizeof(T) + ch * 16;
-        const bool v = (live >> r) & 1;
-        const int d = pa_at<T, DH>(r, ch);
-        cp_async16(ks + d, a.pv.k + (v ? o : 0), v);
-        cp_async16(vs + d, a.pv.v + (v ? o : 0), v);
-      }
-      ++c;
-      if (c < hi) {
-        if (--p.left > 0) ++p.chunk;
-        else p = pa_place(a, pre, c, hi);
-        ask();
-      }
-    }
-    cp_async_commit();
-    return live;
-  }
-};
 
 // Where a (row, head) pair of a unit lies: packed row and query head; false behind the sequence's last row.
 __device__ __forceinline__ bool pa_row(const PagedAttnArgs& a, const RowSpan& rs, const PaPlace& p, int i, int& row, int& head) {
@@ -190,78 +167,340 @@ __device__ __forceinline__ bool pa_row(const PagedAttnArgs& a, const RowSpan& rs
   return true;
 }
 
+// Byte offset of 16-byte chunk c of row r in a [16][DH] tile: chunks are exchanged within groups of eight by the row, so that eight
+// rows' chunks c lie in different banks.
+template <typename T, int DH>
+__device__ __forceinline__ int pa_at(int r, int c) {
+  return r * DH * (int)sizeof(T) + ((c ^ (r & 7)) << 4);
+}
+// The same in a tile of queries; fp32: not exchanged, the second half of a row 16 bytes on (half-warps read one half each).
+template <typename T, int DH>
+__device__ __forceinline__ int pa_q_at(int r, int c) {
+  if constexpr (sizeof(T) == 2) return pa_at<T, DH>(r, c);
+  else return r * PaSmem<T, DH>::Q_ROW + c * 16 + (c >= DH / 8 ? 16 : 0);
+}
+
+// One warp's loads: the rows of its 16 slots of a chunk, K then V, into one stage of its ring; and its part of the queries of a unit
+// that begins with the chunk.
+template <typename T, int DH>
+struct PaLoader {
+  static constexpr int CPR = DH * (int)sizeof(T) / 16;      // 16-byte chunks of a row
+  const PagedAttnArgs& a;
+  const int* pre;
+  int hi, w, lane;
+  PaPlace p;
+  bool first;                   // the next chunk is the run's first of its unit
+  int tile;                     // of the unit that comes next
+  // page ids of this warp's slots: lanes 0 to 15 those of chunk `base`, 16 to 31 of the one behind it; the same two chunks on, under way
+  int base, ids, ids2;
+  __device__ __forceinline__ PaLoader(const PagedAttnArgs& a_, const int* pre_, int hi_, const PaPlace& p_)
+      : a(a_), pre(pre_), hi(hi_), w(threadIdx.x >> 5), lane(threadIdx.x & 31), p(p_), first(true), tile(0) {
+    begin();
+  }
+  __device__ __forceinline__ int ask(int chunk) const {
+    const int j = (chunk + (lane >> 4)) * PA_CHUNK + w * 16 + (lane & 15);
+    return j < p.len ? pg_page(a.pv, p.b, j) : -1;
+  }
+  __device__ __forceinline__ void begin() {
+    base = p.chunk;
+    ids = ask(base);
+    ids2 = ask(base + 2);
+  }
+  // Returns a mask of the rows that are real slots.
+  __device__ __forceinline__ unsigned issue(char* stage, char* q_tiles) {
+    unsigned live = 0;
+    if (p.left > 0) {
+      if (first) {
+        const RowSpan rs = pg_rows(a.pv, a.row_off, p.b, a.max_rows, a.n_rows);
+        char* q_tile = q_tiles + tile * PaSmem<T, DH>::q_tile(a.q_rows);
+        if (++tile == PaSmem<T, DH>::Q_TILES) tile = 0;
+        const int pieces = min(PA_ROWS, rs.n * a.group - p.rt * PA_ROWS) * CPR;
+        for (int i = threadIdx.x; i < pieces; i += PA_THREADS) {
+          int row, head;
+          pa_row(a, rs, p, i / CPR, row, head);
+          cp_async16(smem_u32(q_tile + pa_q_at<T, DH>(i / CPR, i % CPR)), (const T*)a.q + (long long)row * a.ldq + head * DH + (i % CPR) * (16 / (int)sizeof(T)), true);
+        }
+      }
+      const int id = __shfl_sync(0xffffffffu, ids, (p.chunk - base) * 16 + (lane & 15));
+      const int j = p.chunk * PA_CHUNK + w * 16 + (lane & 15);
+      live = __ballot_sync(0xffffffffu, id >= 0) & 0xffffu;
+      const long long off = id < 0 ? 0 : (long long)id * a.pv.page_stride + (long long)(j % a.pv.page) * a.pv.row_stride + (long long)p.kvh * a.pv.head_stride;
+      const uint32_t ks = smem_u32(stage), vs = ks + 16 * DH * (int)sizeof(T);
+#pragma unroll
+      for (int i = 0; i < 16 * CPR / 32; ++i) {
+        const int r = (i * 32 + lane) / CPR, ch = (i * 32 + lane) % CPR;
+        const long long o = __shfl_sync(0xffffffffu, off, r) * (int)sizeof(T) + ch * 16;
+        const bool v = (live >> r) & 1;
+        const int d = pa_at<T, DH>(r, ch);
+        cp_async16(ks + d, a.pv.k + (v ? o : 0), v);
+        cp_async16(vs + d, a.pv.v + (v ? o : 0), v);
+      }
+      first = --p.left == 0;
+      if (first) {
+        p = pa_place(a, pre, p.next(), hi);
+        if (p.left > 0) begin();
+      } else if (++p.chunk == base + 2) {
+        base += 2;
+        ids = ids2;
+        ids2 = ask(base + 2);
+      }
+    }
+    cp_async_commit();
+    return live;
+  }
+};
+
+// The ring of a warp: which stage is next, what is in flight.
+template <typename T, int DH>
+struct PaRing {
+  using S = PaSmem<T, DH>;
+  PaLoader<T, DH> ld;
+  char *q_tiles, *ring;
+  int q_tile_bytes, stage = 0, tile = 0;
+  unsigned live[S::STAGES];     // masks of the stages in flight, oldest first
+  __device__ __forceinline__ PaRing(const PagedAttnArgs& a, const int* pre, int hi, const PaPlace& p, char* smem)
+      : ld(a, pre, hi, p), q_tiles(smem), ring(smem + S::rings(a.q_rows) + (threadIdx.x >> 5) * S::STAGES * S::STAGE), q_tile_bytes(S::q_tile(a.q_rows)) {
+#pragma unroll
+    for (int s = 0; s < S::STAGES - 1; ++s) live[s] = ld.issue(ring + s * S::STAGE, q_tiles);
+    live[S::STAGES - 1] = 0;
+  }
+  // Asks for one chunk more (into the stage that was read last turn) and waits for the oldest; its rows and their mask.
+  __device__ __forceinline__ unsigned turn(char*& rows) {
+    int s = stage + S::STAGES - 1;
+    if (s >= S::STAGES) s -= S::STAGES;
+    __syncwarp();
+    live[S::STAGES - 1] = ld.issue(ring + s * S::STAGE, q_tiles);
+    cp_async_wait<S::STAGES - 1>();
+    __syncwarp();
+    const unsigned mask = live[0];
+#pragma unroll
+    for (int i = 0; i + 1 < S::STAGES; ++i) live[i] = live[i + 1];
+    rows = ring + stage * S::STAGE;
+    if (++stage == S::STAGES) stage = 0;
+    return mask;
+  }
+  // The queries of the unit that begins: there for all warps behind the barrier that follows its first turn.
+  __device__ __forceinline__ const char* queries() {
+    const char* q = q_tiles + tile * q_tile_bytes;
+    if (++tile == S::Q_TILES) tile = 0;
+    return q;
+  }
+};
+
 // e^(x) of the online softmax in log2 units; -inf - -inf (nothing seen yet) counts as nothing.
 __device__ __forceinline__ float pa_scale(float m_old, float m_new) { return m_old == -INFINITY ? 0.f : exp2f(m_old - m_new); }
 
-// Natural log of the sum of exponentials from the maximum in log2 units and the sum; -inf where nothing was seen.
-__device__ __forceinline__ float pa_lse(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f; }
+// A lane's share of a result row: VEC = DH / 32 neighbouring elements, sums o over weights that sum to l.
+template <typename T, int DH>
+__device__ __forceinline__ void pa_write_row(const PagedAttnArgs& a, int row, int head, const float (&o)[DH / 32], float m, float l) {
+  constexpr int VEC = DH / 32;
+  const int lane = threadIdx.x & 31;
+  const float inv = l == 0.f ? 0.f : 1.f / l;                 // (no slot, or all scores -inf: the sums are 0)
+  T* dst = (T*)a.out + (long long)row * a.ldo + head * DH + lane * VEC;
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int e = 0; e < VEC; e += 2) reinterpret_cast<uint32_t*>(dst)[e / 2] = pack_bf16(o[e] * inv, o[e + 1] * inv);
+  } else {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) dst[e] = o[e] * inv;
+  }
+  if (lane == 0) {
+    const long long at = (long long)row * a.hq + head;
+    const float x = l == 0.f ? -INFINITY : m + log2f(l);
+    if (a.lse) a.lse[at] = x * 0.6931471805599453f;
+    if (a.scores) a.row_lse[at] = x;
+  }
+}
+
+// The end of a unit, or of the run's part of it.  The warps' parts are added for merge_rows rows at a time: put(i, n, o, ml) leaves this warp's
+// rows i .. i + n - 1 ([n][DH], pairs of elements exchanged by 4 (row & 3)) and their (m, l); warp w adds row i + w.  A part of a cut unit
+// is noted in cut[] (at most one that begins ahead of the run and one that ends behind it).
+template <typename T, int DH, typename Put>
+__device__ __forceinline__ void pa_finish(const PagedAttnArgs& a, const PaPlace& p, const RowSpan& rs, int lo, PaPlace* cut, char* smem, Put put) {
+  constexpr int VEC = DH / 32;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  float* merge = reinterpret_cast<float*>(smem + PaSmem<T, DH>::merge(a.q_rows));
+  float2* ml = reinterpret_cast<float2*>(smem + PaSmem<T, DH>::ml(a.q_rows, a.merge_rows));
+  const int n_real = min(PA_ROWS, rs.n * a.group - p.rt * PA_ROWS);
+  const bool whole = p.left == p.chunks;
+  const int second = lo >= p.u0 ? 0 : 1, part = 2 * blockIdx.x + second;
+  if (!whole && threadIdx.x == 0) cut[second] = p;
+  for (int i = 0; i < n_real; i += a.merge_rows) {
+    if (i > 0) __syncthreads();
+    put(i, a.merge_rows, merge + w * a.merge_rows * DH, ml + w * a.merge_rows);
+    __syncthreads();
+    if (w < a.merge_rows && i + w < n_real) {
+      float m = -INFINITY, l = 0.f, o[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) o[e] = 0.f;
+#pragma unroll
+      for (int k = 0; k < PA_WARPS; ++k) m = fmaxf(m, ml[k * a.merge_rows + w].x);
+#pragma unroll
+      for (int k = 0; k < PA_WARPS; ++k) {
+        const float2 x = ml[k * a.merge_rows + w];
+        const float f = pa_scale(x.x, m);
+        l = fmaf(x.y, f, l);
+        const float* src = merge + (k * a.merge_rows + w) * DH;
+#pragma unroll
+        for (int e = 0; e < VEC; e += 2) {
+          const float2 y = *reinterpret_cast<const float2*>(src + (((lane * VEC + e) / 2) ^ (4 * w)) * 2);
+          o[e] = fmaf(y.x, f, o[e]);
+          o[e + 1] = fmaf(y.y, f, o[e + 1]);
+        }
+      }
+      if (whole) {
+        int row, head;
+        pa_row(a, rs, p, i + w, row, head);
+        pa_write_row<T, DH>(a, row, head, o, m, l);
+      } else {
+        float* dst = a.part_o + ((long long)part * PA_ROWS + i + w) * DH + lane * VEC;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) dst[e] = o[e];
+        if (lane == 0) a.part_ml[part * PA_ROWS + i + w] = make_float2(m, l);
+      }
+    }
+  }
+}
+
+// The end of the run: its parts of cut units are there; the last CTA of a unit to say so adds them all, in their order.  A warp takes a
+// row at a time, 32 parts' (m, l) on its lanes and PA_AHEAD parts' o under way; the code is short because it is fetched cold.
+constexpr int PA_AHEAD = 16;
+template <typename T, int DH>
+__device__ __forceinline__ void pa_join(const PagedAttnArgs& a, const PaDeal& deal, const PaPlace* cut) {
+  constexpr int VEC = DH / 32;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  __shared__ int parts[2][3];                      // of the unit that is this CTA's to add: first CTA and its part, last CTA
+  cp_async_wait<0>();
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    const PaPlace& p = cut[threadIdx.x];
+    int i0 = 0, i1 = -1, second = 0;
+    if (p.left > 0) {
+      i0 = deal.owner(p.u0);                       // CTAs i0 .. i1 have a part each
+      i1 = deal.owner(p.u0 + p.chunks - 1);
+      second = deal.run(i0) < p.u0 ? 1 : 0;        // the unit begins in the first one's run: its second part
+      __threadfence();
+      if (atomicAdd(a.arrived + i0, 1u) == (unsigned)(i1 - i0)) a.arrived[i0] = 0;
+      else i1 = -1;
+      __threadfence();
+    }
+    parts[threadIdx.x][0] = i0;
+    parts[threadIdx.x][1] = second;
+    parts[threadIdx.x][2] = i1;
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int which = 0; which < 2; ++which) {
+    const int i0 = parts[which][0], n = parts[which][2] - i0 + 1;
+    if (n <= 0) continue;
+    const PaPlace p = cut[which];
+    const RowSpan rs = pg_rows(a.pv, a.row_off, p.b, a.max_rows, a.n_rows);
+    const int n_real = min(PA_ROWS, rs.n * a.group - p.rt * PA_ROWS);
+#pragma unroll 1
+    for (int r = w; r < n_real; r += PA_WARPS) {
+      float m = -INFINITY, l = 0.f, o[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) o[e] = 0.f;
+#pragma unroll 1
+      for (int k0 = 0; k0 < n; k0 += 32) {
+        const int k = min(k0 + lane, n - 1);
+        const int slot = (2 * (i0 + k) + (k == 0 ? parts[which][1] : 0)) * PA_ROWS + r;
+        const float2 x = __ldcg(a.part_ml + slot);
+        const float top = fmaxf(m, warp_max(x.x)), f0 = pa_scale(m, top);
+        const float f = k0 + lane < n ? pa_scale(x.x, top) : 0.f;
+        m = top;
+        l = l * f0 + warp_sum(x.y * f);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) o[e] *= f0;
+#pragma unroll 1
+        for (int q = 0; q < 32 && k0 + q < n; q += PA_AHEAD) {
+          float y[PA_AHEAD][VEC];
+#pragma unroll
+          for (int i = 0; i < PA_AHEAD; ++i) {
+            const float* src = a.part_o + (long long)__shfl_sync(0xffffffffu, slot, q + i) * DH + lane * VEC;
+            if constexpr (VEC == 4) {
+              const float4 z = __ldcg(reinterpret_cast<const float4*>(src));
+              y[i][0] = z.x; y[i][1] = z.y; y[i][2] = z.z; y[i][3] = z.w;
+            } else {
+              const float2 z = __ldcg(reinterpret_cast<const float2*>(src));
+              y[i][0] = z.x; y[i][1] = z.y;
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < PA_AHEAD; ++i) {
+            const float g = __shfl_sync(0xffffffffu, f, q + i);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) o[e] = fmaf(y[i][e], g, o[e]);
+          }
+        }
+      }
+      int row, head;
+      pa_row(a, rs, p, r, row, head);
+      pa_write_row<T, DH>(a, row, head, o, m, l);
+    }
+  }
+}
+
+// Rows of sequences without a slot: 0.  (The grid's CTAs take the sequences in turn.)
+template <typename T, int DH>
+__device__ __forceinline__ void pa_empty(const PagedAttnArgs& a, const int* pre) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  for (int b = blockIdx.x; b < a.pv.batch; b += gridDim.x) {
+    if (pre[b + 1] > pre[b]) continue;
+    const RowSpan rs = pg_rows(a.pv, a.row_off, b, a.max_rows, a.n_rows);
+    const float o[DH / 32] = {};
+    for (int i = w; i < rs.n * a.hq; i += PA_WARPS) pa_write_row<T, DH>(a, rs.first + i / a.hq, i % a.hq, o, -INFINITY, 0.f);
+  }
+}
 
 // ---- bf16: tensor cores --------------------------------------------------------------------------------------------------
 // Softmax weights are fed to the P V product as the sum of two bf16 numbers (16 bits of mantissa): the tensor pipe has the time,
 // and the output is then as exact as one with fp32 weights.
 template <int DH>
-__global__ void __launch_bounds__(PA_WARPS * 32, 2) k_paged_attn_mma(const PagedAttnArgs a) {
+__global__ void __launch_bounds__(PA_THREADS, 2) k_paged_attn_mma(const PagedAttnArgs a) {
   extern __shared__ __align__(128) char pa_smem[];
-  constexpr int SB = pa_stage_bytes<bf16, DH>();
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  char* ring = pa_smem + w * PA_STAGES * SB;
-  float* merge = reinterpret_cast<float*>(pa_smem + PA_WARPS * PA_STAGES * SB);
-  float2* ml_s = reinterpret_cast<float2*>(merge + 2 * 8 * DH);       // [warp][16]
-  int* pre = reinterpret_cast<int*>(ml_s + PA_WARPS * PA_ROWS);
-  __shared__ int warp_sums[PA_WARPS];
+  int* pre = reinterpret_cast<int*>(pa_smem + PaSmem<bf16, DH>::pre(a.q_rows, a.merge_rows));
   pdl_begin();
-  pa_prefix<PA_WARPS * 32>(a, pre, warp_sums);
-  const int total = pre[a.pv.batch];
-  const int n_cta = pa_ctas(total, a.n_cta);
-  if ((int)blockIdx.x >= n_cta) return;
-  const int lo = pa_run(total, blockIdx.x, n_cta), hi = pa_run(total, blockIdx.x + 1, n_cta);
+  pa_prefix(a, pre);
+  pa_empty<bf16, DH>(a, pre);
+  const PaDeal deal(pre[a.pv.batch], a.n_cta);
+  if ((int)blockIdx.x >= deal.n) return;
+  const int lo = deal.run(blockIdx.x), hi = deal.run(blockIdx.x + 1);
+  PaPlace p = pa_place(a, pre, lo, hi);
+  if (p.left == 0) return;
+  __shared__ PaPlace cut[2];
+  if (threadIdx.x < 2) cut[threadIdx.x].left = 0;
 
-  PaLoader<bf16, DH> ld(a, pre, lo, hi, w, lane);
-  unsigned live[PA_STAGES];                   // masks of the stages in flight, oldest first
-#pragma unroll
-  for (int s = 0; s < PA_STAGES - 1; ++s) live[s] = ld.issue(ring + s * SB);
-  live[PA_STAGES - 1] = 0;
-
-  int c = lo, stage = 0;
-  while (c < hi) {
+  PaRing<bf16, DH> ring(a, pre, hi, p, pa_smem);
+  for (; p.left > 0; p = pa_place(a, pre, p.next(), hi)) {
     // ---- a unit, or the part of it that belongs to this run
-    const PaPlace p = pa_place(a, pre, c, hi);
     const RowSpan rs = pg_rows(a.pv, a.row_off, p.b, a.max_rows, a.n_rows);
-    uint32_t qf[DH / 16][4];
+    const int n_real = min(PA_ROWS, rs.n * a.group - p.rt * PA_ROWS);
     int row[2], head[2];
     bool real[2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      real[h] = pa_row(a, rs, p, g + 8 * h, row[h], head[h]);
-      const uint32_t* src = reinterpret_cast<const uint32_t*>((const bf16*)a.q + (real[h] ? (long long)row[h] * a.ldq + head[h] * DH : 0)) + t;
-#pragma unroll
-      for (int kk = 0; kk < DH / 16; ++kk) {
-        qf[kk][h] = real[h] ? src[kk * 8] : 0u;
-        qf[kk][2 + h] = real[h] ? src[kk * 8 + 4] : 0u;
-      }
-    }
+    for (int h = 0; h < 2; ++h) real[h] = pa_row(a, rs, p, g + 8 * h, row[h], head[h]);
+    uint32_t qf[DH / 16][4];
     float o[DH / 8][4];
 #pragma unroll
     for (int i = 0; i < DH / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 
     for (int k = 0; k < p.left; ++k) {
-      // the next chunk's rows into the stage that was read last turn
-      {
-        int s = stage + PA_STAGES - 1;
-        if (s >= PA_STAGES) s -= PA_STAGES;
-        __syncwarp();
-        live[PA_STAGES - 1] = ld.issue(ring + s * SB);
-      }
-      cp_async_wait<PA_STAGES - 1>();
-      __syncwarp();
-      const unsigned mask = live[0];
+      char* rows;
+      const unsigned mask = ring.turn(rows);
+      if (k == 0) {
+        __syncthreads();                        // all warps' parts of the queries are there (and the last unit's parts have been read)
+        const int r = min((lane & 7) + ((lane >> 3) & 1) * 8, n_real - 1);      // rows that are none repeat the last one
+        const uint32_t qs = smem_u32(ring.queries());
 #pragma unroll
-      for (int s = 0; s + 1 < PA_STAGES; ++s) live[s] = live[s + 1];
-      const uint32_t ks = smem_u32(ring + stage * SB), vs = ks + 16 * DH * 2;
-      if (++stage == PA_STAGES) stage = 0;
+        for (int kk = 0; kk < DH / 16; ++kk) ldsm_x4(qs + pa_q_at<bf16, DH>(r, kk * 2 + (lane >> 4)), qf[kk][0], qf[kk][1], qf[kk][2], qf[kk][3]);
+        __syncthreads();                        // before anyone asks for further queries in their place
+      }
       const int j0 = (p.chunk + k) * PA_CHUNK + w * 16;
       if (mask == 0 && (!a.scores || j0 >= p.len)) continue;
+      const uint32_t ks = smem_u32(rows), vs = ks + 16 * DH * 2;
       // S = Q K^T: 16 rows x 16 slots
       float s[2][4];
 #pragma unroll
@@ -339,190 +578,105 @@ __global__ void __launch_bounds__(PA_WARPS * 32, 2) k_paged_attn_mma(const Paged
         mma_bf16(o[nt + 1], lo_[0], lo_[1], lo_[2], lo_[3], b2, b3);
       }
     }
-
-    // ---- the four warps' parts of the unit: to one maximum, then added in pairs (half of the rows at a time)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
       l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-      if (t == 0) ml_s[w * PA_ROWS + g + 8 * h] = make_float2(m[h], l[h]);
     }
-    __syncthreads();
-    float mt[2], lt[2];
+    pa_finish<bf16, DH>(a, p, rs, lo, cut, pa_smem, [&](int i0, int n, float* dst, float2* ml) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      mt[h] = -INFINITY;
-      lt[h] = 0.f;
+      for (int h = 0; h < 2; ++h) {
+        const int r = g + 8 * h - i0;
+        if (r < 0 || r >= n) continue;
 #pragma unroll
-      for (int i = 0; i < PA_WARPS; ++i) mt[h] = fmaxf(mt[h], ml_s[i * PA_ROWS + g + 8 * h].x);
-#pragma unroll
-      for (int i = 0; i < PA_WARPS; ++i) {
-        const float2 x = ml_s[i * PA_ROWS + g + 8 * h];
-        lt[h] += x.y * pa_scale(x.x, mt[h]);
+        for (int i = 0; i < DH / 8; ++i) *reinterpret_cast<float2*>(dst + r * DH + ((i * 4 + t) ^ (4 * r)) * 2) = make_float2(o[i][2 * h], o[i][2 * h + 1]);
+        if (t == 0) ml[r] = make_float2(m[h], l[h]);
       }
-      const float f = pa_scale(m[h], mt[h]);
-#pragma unroll
-      for (int i = 0; i < DH / 8; ++i) {
-        o[i][2 * h] *= f;
-        o[i][2 * h + 1] *= f;
-      }
-    }
-    const int n_real = rs.n * a.group - p.rt * PA_ROWS;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (8 * h >= n_real) break;               // (the same for the whole block)
-#pragma unroll
-      for (int step = 0; step < 2; ++step) {
-        const int half = 2 >> step;             // warps [half, 2 half) hand over to [0, half)
-        if (w >= half && w < 2 * half) {
-          float2* dst = reinterpret_cast<float2*>(merge + ((w - half) * 8 + g) * DH);
-#pragma unroll
-          for (int i = 0; i < DH / 8; ++i) dst[(i * 4 + t) ^ g] = make_float2(o[i][2 * h], o[i][2 * h + 1]);
-        }
-        __syncthreads();
-        if (w < half) {
-          const float2* src = reinterpret_cast<const float2*>(merge + (w * 8 + g) * DH);
-#pragma unroll
-          for (int i = 0; i < DH / 8; ++i) {
-            const float2 x = src[(i * 4 + t) ^ g];
-            o[i][2 * h] += x.x;
-            o[i][2 * h + 1] += x.y;
-          }
-        }
-        __syncthreads();
-      }
-    }
-    if (w == 0) {
-      if (p.left == p.chunks) {                 // the whole unit: the result
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          if (real[h]) {
-            const float inv = 1.f / lt[h];
-            uint32_t* dst = reinterpret_cast<uint32_t*>((bf16*)a.out + (long long)row[h] * a.ldo + head[h] * DH) + t;
-#pragma unroll
-            for (int i = 0; i < DH / 8; ++i) dst[i * 4] = lt[h] == 0.f ? 0u : pack_bf16(o[i][2 * h] * inv, o[i][2 * h + 1] * inv);
-            if (t == 0) {
-              const long long at = (long long)row[h] * a.hq + head[h];
-              if (a.lse) a.lse[at] = pa_lse(mt[h], lt[h]);
-              if (a.scores) a.row_ml[at] = make_float2(mt[h], lt[h]);
-            }
-          }
-      } else {
-        const int part = 2 * blockIdx.x + (c == lo ? 0 : 1);
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          if (real[h]) {
-            float2* dst = reinterpret_cast<float2*>(a.part_o + ((long long)part * PA_ROWS + g + 8 * h) * DH) + t;
-#pragma unroll
-            for (int i = 0; i < DH / 8; ++i) dst[i * 4] = make_float2(o[i][2 * h], o[i][2 * h + 1]);
-            if (t == 0) a.part_ml[part * PA_ROWS + g + 8 * h] = make_float2(mt[h], lt[h]);
-          }
-      }
-    }
-    c += p.left;
+    });
   }
-  cp_async_wait<0>();
+  pa_join<bf16, DH>(a, deal, cut);
 }
 
 // ---- fp32: CUDA cores ----------------------------------------------------------------------------------------------------
-// Scores: a lane takes one slot and half of the dimensions; P V: a lane takes DH / 32 dimensions.  16 rows cost 256 FMAs a lane and
-// 16 slots either way, a third of the time the bytes take.
-template <int DH>
-__global__ void __launch_bounds__(PA_WARPS * 32) k_paged_attn_simt(const PagedAttnArgs a) {
+// Scores: a lane takes one slot and half of the dimensions; P V: a lane takes DH / 32 dimensions.  A kernel for every power of two of
+// rows: the work a slot costs goes with the rows, and a branch a row and slot (16 of them with one real row) took ten times the bytes' time.
+template <int DH, int NR>
+__global__ void __launch_bounds__(PA_THREADS) k_paged_attn_simt(const PagedAttnArgs a) {
   extern __shared__ __align__(128) char pa_smem[];
-  constexpr int SB = pa_stage_bytes<float, DH>();
   constexpr int VEC = DH / 32;                  // dimensions of a lane in P V
-  constexpr int HALF = DH / 2;
-  constexpr int LDQ = DH + 4;                   // second half of a query 16 bytes on: the two half-warps read different banks
+  constexpr int PARTS = NR <= 2 ? 4 : 1;        // independent sums of a score (few rows: the chain of FMAs would be the time)
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  char* ring = pa_smem + w * PA_STAGES * SB;
-  float* merge = reinterpret_cast<float*>(pa_smem + PA_WARPS * PA_STAGES * SB);
-  float2* ml_s = reinterpret_cast<float2*>(merge + 2 * 8 * DH);
-  float* qs = reinterpret_cast<float*>(ml_s + PA_WARPS * PA_ROWS);    // [16][DH + 4]
-  int* pre = reinterpret_cast<int*>(qs + PA_ROWS * LDQ);
-  __shared__ int warp_sums[PA_WARPS];
+  int* pre = reinterpret_cast<int*>(pa_smem + PaSmem<float, DH>::pre(a.q_rows, a.merge_rows));
   pdl_begin();
-  pa_prefix<PA_WARPS * 32>(a, pre, warp_sums);
-  const int total = pre[a.pv.batch];
-  const int n_cta = pa_ctas(total, a.n_cta);
-  if ((int)blockIdx.x >= n_cta) return;
-  const int lo = pa_run(total, blockIdx.x, n_cta), hi = pa_run(total, blockIdx.x + 1, n_cta);
+  pa_prefix(a, pre);
+  pa_empty<float, DH>(a, pre);
+  const PaDeal deal(pre[a.pv.batch], a.n_cta);
+  if ((int)blockIdx.x >= deal.n) return;
+  const int lo = deal.run(blockIdx.x), hi = deal.run(blockIdx.x + 1);
+  PaPlace p = pa_place(a, pre, lo, hi);
+  if (p.left == 0) return;
+  __shared__ PaPlace cut[2];
+  if (threadIdx.x < 2) cut[threadIdx.x].left = 0;
 
-  PaLoader<float, DH> ld(a, pre, lo, hi, w, lane);
-  unsigned live[PA_STAGES];
-#pragma unroll
-  for (int s = 0; s < PA_STAGES - 1; ++s) live[s] = ld.issue(ring + s * SB);
-  live[PA_STAGES - 1] = 0;
-
-  int c = lo, stage = 0;
+  PaRing<float, DH> ring(a, pre, hi, p, pa_smem);
   const int key = lane & 15, half = lane >> 4;
-  while (c < hi) {
-    const PaPlace p = pa_place(a, pre, c, hi);
+  for (; p.left > 0; p = pa_place(a, pre, p.next(), hi)) {
     const RowSpan rs = pg_rows(a.pv, a.row_off, p.b, a.max_rows, a.n_rows);
     const int nr = min(PA_ROWS, rs.n * a.group - p.rt * PA_ROWS);
-    for (int i = threadIdx.x; i < nr * DH; i += PA_WARPS * 32) {
-      const int r = i / DH, d = i % DH;
-      int row, head;
-      pa_row(a, rs, p, r, row, head);
-      qs[r * LDQ + d + (d >= HALF ? 4 : 0)] = ((const float*)a.q)[(long long)row * a.ldq + head * DH + d];
-    }
-    __syncthreads();
-    float o[PA_ROWS][VEC], m[PA_ROWS], l[PA_ROWS];       // m: the same in all lanes; l: this lane's slots
+    float o[NR][VEC], m[NR], l[NR];             // m: the same in all lanes; l: this lane's slots
 #pragma unroll
-    for (int r = 0; r < PA_ROWS; ++r) {
+    for (int r = 0; r < NR; ++r) {
       m[r] = -INFINITY;
       l[r] = 0.f;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) o[r][e] = 0.f;
     }
+    const char* qs = nullptr;
     for (int k = 0; k < p.left; ++k) {
-      {
-        int s = stage + PA_STAGES - 1;
-        if (s >= PA_STAGES) s -= PA_STAGES;
-        __syncwarp();
-        live[PA_STAGES - 1] = ld.issue(ring + s * SB);
+      char* rows;
+      const unsigned mask = ring.turn(rows);
+      if (k == 0) {
+        __syncthreads();
+        qs = ring.queries();
       }
-      cp_async_wait<PA_STAGES - 1>();
-      __syncwarp();
-      const unsigned mask = live[0];
-#pragma unroll
-      for (int s = 0; s + 1 < PA_STAGES; ++s) live[s] = live[s + 1];
-      const char* ks = ring + stage * SB;
-      const char* vs = ks + 16 * DH * 4;
-      if (++stage == PA_STAGES) stage = 0;
       const int j = (p.chunk + k) * PA_CHUNK + w * 16 + key;
       if (mask == 0 && (!a.scores || j - key >= p.len)) continue;
-      float s[PA_ROWS];
+      const char* ks = rows;
+      const char* vs = ks + 16 * DH * 4;
+      float s[NR][PARTS];
 #pragma unroll
-      for (int r = 0; r < PA_ROWS; ++r) s[r] = 0.f;
+      for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int x = 0; x < PARTS; ++x) s[r][x] = 0.f;
 #pragma unroll 4
-      for (int ch = 0; ch < HALF / 4; ++ch) {
-        const float4 kv = *reinterpret_cast<const float4*>(ks + pa_at<float, DH>(key, half * (HALF / 4) + ch));
+      for (int ch = 0; ch < DH / 8; ++ch) {
+        const float4 kv = *reinterpret_cast<const float4*>(ks + pa_at<float, DH>(key, half * (DH / 8) + ch));
 #pragma unroll
-        for (int r = 0; r < PA_ROWS; ++r)
-          if (r < nr) {
-            const float4 qv = *reinterpret_cast<const float4*>(qs + r * LDQ + half * (HALF + 4) + ch * 4);
-            s[r] = fmaf(qv.x, kv.x, fmaf(qv.y, kv.y, fmaf(qv.z, kv.z, fmaf(qv.w, kv.w, s[r]))));
-          }
-      }
-#pragma unroll
-      for (int r = 0; r < PA_ROWS; ++r)
-        if (r < nr) {
-          s[r] += __shfl_xor_sync(0xffffffffu, s[r], 16);
-          s[r] = (mask >> key) & 1 ? s[r] * a.scale_log2 : -INFINITY;
-          if (a.scores && half == 0 && j < p.len) {
-            int row, head;
-            pa_row(a, rs, p, r, row, head);
-            a.scores[((long long)row * a.hq + head) * pg_capacity(a.pv) + j] = s[r];
-          }
-          const float m_new = fmaxf(m[r], warp_max(s[r]));
-          const float corr = pa_scale(m[r], m_new);
-          m[r] = m_new;
-          s[r] = s[r] == -INFINITY ? 0.f : exp2f(s[r] - m_new);
-          l[r] = l[r] * corr + s[r];
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) o[r][e] *= corr;
+        for (int r = 0; r < NR; ++r) {
+          const float4 qv = *reinterpret_cast<const float4*>(qs + pa_q_at<float, DH>(r < nr ? r : 0, half * (DH / 8) + ch));
+          float& x = s[r][ch % PARTS];
+          x = fmaf(qv.x, kv.x, fmaf(qv.y, kv.y, fmaf(qv.z, kv.z, fmaf(qv.w, kv.w, x))));
         }
+      }
+      float pr[NR];
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        float x = PARTS == 4 ? (s[r][0] + s[r][1 % PARTS]) + (s[r][2 % PARTS] + s[r][3 % PARTS]) : s[r][0];
+        x += __shfl_xor_sync(0xffffffffu, x, 16);
+        x = (mask >> key) & 1 ? x * a.scale_log2 : -INFINITY;
+        if (a.scores && half == 0 && j < p.len && r < nr) {
+          int row, head;
+          pa_row(a, rs, p, r, row, head);
+          a.scores[((long long)row * a.hq + head) * pg_capacity(a.pv) + j] = x;
+        }
+        const float m_new = fmaxf(m[r], warp_max(x));
+        const float corr = pa_scale(m[r], m_new);
+        m[r] = m_new;
+        pr[r] = x == -INFINITY ? 0.f : exp2f(x - m_new);
+        l[r] = l[r] * corr + pr[r];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) o[r][e] *= corr;
+      }
 #pragma unroll 4
       for (int i = 0; i < 16; ++i) {
         float v[VEC];
@@ -534,197 +688,49 @@ __global__ void __launch_bounds__(PA_WARPS * 32) k_paged_attn_simt(const PagedAt
           v[0] = x.x; v[1] = x.y;
         }
 #pragma unroll
-        for (int r = 0; r < PA_ROWS; ++r)
-          if (r < nr) {
-            const float pr = __shfl_sync(0xffffffffu, s[r], i);
+        for (int r = 0; r < NR; ++r) {
+          const float x = __shfl_sync(0xffffffffu, pr[r], i);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) o[r][e] = fmaf(pr, v[e], o[r][e]);
-          }
-      }
-    }
-    // ---- join the four warps
-#pragma unroll
-    for (int r = 0; r < PA_ROWS; ++r)
-      if (r < nr) {
-        const float s = warp_sum(half == 0 ? l[r] : 0.f);
-        if (lane == 0) ml_s[w * PA_ROWS + r] = make_float2(m[r], s);
-      }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < PA_ROWS; ++r)
-      if (r < nr) {
-        float mt = -INFINITY, lt = 0.f;
-#pragma unroll
-        for (int i = 0; i < PA_WARPS; ++i) mt = fmaxf(mt, ml_s[i * PA_ROWS + r].x);
-#pragma unroll
-        for (int i = 0; i < PA_WARPS; ++i) lt += ml_s[i * PA_ROWS + r].y * pa_scale(ml_s[i * PA_ROWS + r].x, mt);
-        const float f = pa_scale(m[r], mt);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) o[r][e] *= f;
-        m[r] = mt;
-        l[r] = lt;
-      }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (8 * h >= nr) break;
-#pragma unroll
-      for (int step = 0; step < 2; ++step) {
-        const int n = 2 >> step;
-        if (w >= n && w < 2 * n)
-#pragma unroll
-          for (int r = 0; r < 8; ++r)
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) merge[((w - n) * 8 + r) * DH + lane * VEC + e] = o[8 * h + r][e];
-        __syncthreads();
-        if (w < n)
-#pragma unroll
-          for (int r = 0; r < 8; ++r)
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) o[8 * h + r][e] += merge[(w * 8 + r) * DH + lane * VEC + e];
-        __syncthreads();
-      }
-    }
-    if (w == 0) {
-      const bool whole = p.left == p.chunks;
-      const int part = 2 * blockIdx.x + (c == lo ? 0 : 1);
-#pragma unroll
-      for (int r = 0; r < PA_ROWS; ++r)
-        if (r < nr) {
-          int row, head;
-          pa_row(a, rs, p, r, row, head);
-          float* dst = whole ? (float*)a.out + (long long)row * a.ldo + head * DH : a.part_o + ((long long)part * PA_ROWS + r) * DH;
-          const float inv = whole ? (l[r] == 0.f ? 0.f : 1.f / l[r]) : 1.f;
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) dst[lane * VEC + e] = o[r][e] * inv;
-          if (lane == 0) {
-            if (whole) {
-              const long long at = (long long)row * a.hq + head;
-              if (a.lse) a.lse[at] = pa_lse(m[r], l[r]);
-              if (a.scores) a.row_ml[at] = make_float2(m[r], l[r]);
-            } else {
-              a.part_ml[part * PA_ROWS + r] = make_float2(m[r], l[r]);
-            }
-          }
+          for (int e = 0; e < VEC; ++e) o[r][e] = fmaf(x, v[e], o[r][e]);
         }
+      }
     }
-    c += p.left;
+#pragma unroll
+    for (int r = 0; r < NR; ++r) l[r] = warp_sum(half == 0 ? l[r] : 0.f);
+    pa_finish<float, DH>(a, p, rs, lo, cut, pa_smem, [&](int i0, int n, float* dst, float2* ml) {
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        const int i = r - i0;
+        if (i < 0 || i >= n) continue;
+#pragma unroll
+        for (int e = 0; e < VEC; e += 2) *reinterpret_cast<float2*>(dst + i * DH + (((lane * VEC + e) / 2) ^ (4 * i)) * 2) = make_float2(o[r][e], o[r][e + 1]);
+        if (lane == 0) ml[i] = make_float2(m[r], l[r]);
+      }
+    });
   }
-  cp_async_wait<0>();
+  pa_join<float, DH>(a, deal, cut);
 }
 
-// ---- join ----------------------------------------------------------------------------------------------------------------
-// The parts of unit (b, kvh, rt): CTAs first..last of the attention kernel's grid hold one each.
-struct PaParts {
-  int first, last, u0, total, n_cta;
-  __device__ __forceinline__ int slot(int i) const { return 2 * i + (pa_run(total, i, n_cta) >= u0 ? 0 : 1); }
-};
-__device__ __forceinline__ PaParts pa_parts(const PagedAttnArgs& a, const int* pre, int b, int unit, int chunks) {
-  PaParts p;
-  p.total = pre[a.pv.batch];
-  p.n_cta = pa_ctas(p.total, a.n_cta);
-  p.u0 = pre[b] + unit * chunks;
-  p.first = pa_owner(p.total, p.u0, p.n_cta);
-  p.last = pa_owner(p.total, p.u0 + chunks - 1, p.n_cta);
-  return p;
-}
-
-// Blocks [0, join_blocks): one (unit, row) each, the warps take its parts in turn.  The others: PJ_KEYS slots of one (sequence, KV head) each, the
-// rows' weights there from the scores, which were left in log2 units.
-template <typename T, int DH>
-__global__ void __launch_bounds__(PJ_THREADS) k_paged_join(const PagedAttnArgs a, int tiles, int rows_tile, int join_blocks, int key_blocks) {
-  __shared__ int pre[PA_MAX_BATCH + 1];
-  __shared__ int warp_sums[PJ_THREADS / 32];
-  __shared__ float acc[PJ_THREADS / 32][DH];
-  constexpr int VEC = DH / 32, NW = PJ_THREADS / 32;
-  extern __shared__ float lse2[];                 // [max_rows * group] (weights blocks)
+// ---- gathered weights ----------------------------------------------------------------------------------------------------
+// PW_KEYS slots of one (sequence, KV head) a block, from the scores that the kernel above left: e^{s - lse} of all rows and heads of the group.
+__global__ void __launch_bounds__(PW_THREADS) k_paged_weights(const PagedAttnArgs a, int key_blocks) {
+  extern __shared__ float lse2[];                 // [max_rows * group]
   pdl_begin();
-  pa_prefix<PJ_THREADS>(a, pre, warp_sums);
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  if ((int)blockIdx.x < join_blocks) {
-    const int i = blockIdx.x % rows_tile;
-    int u = blockIdx.x / rows_tile;
-    PaPlace p;
-    p.rt = u % tiles;
-    u /= tiles;
-    p.kvh = u % a.pv.hkv;
-    p.b = u / a.pv.hkv;
-    const RowSpan rs = pg_rows(a.pv, a.row_off, p.b, a.max_rows, a.n_rows);
-    int row, head;
-    if (!pa_row(a, rs, p, i, row, head)) return;
-    const int chunks = pa_chunks(pg_len(a.pv, a.lens, p.b));
-    T* out = (T*)a.out + (long long)row * a.ldo + head * DH;
-    const long long at = (long long)row * a.hq + head;
-    if (chunks == 0) {                            // no slot: nothing seen
-      if (threadIdx.x < DH) out[threadIdx.x] = from_f<T>(0.f);
-      if (threadIdx.x == 0 && a.lse) a.lse[at] = -INFINITY;
-      return;
-    }
-    const int my_tiles = (rs.n * a.group + PA_ROWS - 1) / PA_ROWS;
-    const PaParts pt = pa_parts(a, pre, p.b, p.kvh * my_tiles + p.rt, chunks);
-    if (pt.first == pt.last) return;              // one CTA had it whole and wrote the result
-    float m = -INFINITY;
-    for (int k = pt.first + lane; k <= pt.last; k += 32) m = fmaxf(m, a.part_ml[pt.slot(k) * PA_ROWS + i].x);
-    m = warp_max(m);
-    float l = 0.f, o[VEC];
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) o[e] = 0.f;
-#pragma unroll 4
-    for (int k = pt.first + w; k <= pt.last; k += NW) {
-      const int s = pt.slot(k) * PA_ROWS + i;
-      const float2 ml = a.part_ml[s];
-      const float f = pa_scale(ml.x, m);
-      const float* src = a.part_o + (long long)s * DH + lane * VEC;
-      l += ml.y * f;
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) o[e] = fmaf(src[e], f, o[e]);
-    }
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) acc[w][lane * VEC + e] = o[e];
-    float* ls = reinterpret_cast<float*>(warp_sums);
-    if (lane == 0) ls[w] = l;
-    __syncthreads();
-    float lt = 0.f;
-#pragma unroll
-    for (int k = 0; k < NW; ++k) lt += ls[k];
-    if (threadIdx.x < DH) {
-      float s = 0.f;
-#pragma unroll
-      for (int k = 0; k < NW; ++k) s += acc[k][threadIdx.x];
-      out[threadIdx.x] = from_f<T>(lt == 0.f ? 0.f : s / lt);
-    }
-    if (threadIdx.x == 0 && a.lse) a.lse[at] = pa_lse(m, lt);
-    return;
-  }
-  // ---- gathered weights
-  int u = blockIdx.x - join_blocks;
-  const int j0 = (u % key_blocks) * PJ_KEYS;
+  int u = blockIdx.x;
+  const int j0 = (u % key_blocks) * PW_KEYS;
   u /= key_blocks;
   const int kvh = u % a.pv.hkv, b = u / a.pv.hkv;
-  const int len = pg_len(a.pv, a.lens, b), chunks = pa_chunks(len), cap = pg_capacity(a.pv);
+  const int len = pg_len(a.pv, a.lens[b]), cap = pg_capacity(a.pv);
   if (j0 >= len) return;
   const RowSpan rs = pg_rows(a.pv, a.row_off, b, a.max_rows, a.n_rows);
-  const int n = rs.n * a.group, my_tiles = (n + PA_ROWS - 1) / PA_ROWS;
-  for (int x = w; x < n; x += NW) {
-    const PaParts pt = pa_parts(a, pre, b, kvh * my_tiles + x / PA_ROWS, chunks);
-    float m = -INFINITY, l = 0.f;
-    if (pt.first == pt.last) {
-      const float2 ml = a.row_ml[(long long)(rs.first + x / a.group) * a.hq + kvh * a.group + x % a.group];
-      m = ml.x;
-      l = ml.y;
-    } else {
-      for (int k = pt.first + lane; k <= pt.last; k += 32) m = fmaxf(m, a.part_ml[pt.slot(k) * PA_ROWS + x % PA_ROWS].x);
-      m = warp_max(m);
-      for (int k = pt.first + lane; k <= pt.last; k += 32) {
-        const float2 ml = a.part_ml[pt.slot(k) * PA_ROWS + x % PA_ROWS];
-        l += ml.y * pa_scale(ml.x, m);
-      }
-      l = warp_sum(l);
-    }
-    if (lane == 0) lse2[x] = l == 0.f ? INFINITY : m + log2f(l);
+  const int n = rs.n * a.group;
+  for (int x = threadIdx.x; x < n; x += PW_THREADS) {
+    const float l = a.row_lse[(long long)(rs.first + x / a.group) * a.hq + kvh * a.group + x % a.group];
+    lse2[x] = l == -INFINITY ? INFINITY : l;      // a row that saw nothing has no weight
   }
   __syncthreads();
   const long long base = ((long long)b * a.pv.hkv + kvh) * cap;
-  for (int j = j0 + threadIdx.x; j < min(j0 + PJ_KEYS, len); j += PJ_THREADS) {
+  for (int j = j0 + threadIdx.x; j < min(j0 + PW_KEYS, len); j += PW_THREADS) {
     float s = a.weights_in ? a.weights_in[base + j] : 0.f;
     for (int x = 0; x < n; ++x)
       s += exp2f(a.scores[((long long)(rs.first + x / a.group) * a.hq + kvh * a.group + x % a.group) * cap + j] - lse2[x]);

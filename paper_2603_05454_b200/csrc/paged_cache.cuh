@@ -30,7 +30,7 @@ __global__ void __launch_bounds__(PP_THREADS) k_paged_append(const PagedAppendAr
   if ((int)blockIdx.x == a.n_rows) {
     for (int b = threadIdx.x; b < B; b += PP_THREADS) {
       const RowSpan rs = pg_rows(a.pv, a.row_off, b, a.max_rows, a.n_rows);
-      const int n = pg_len(a.pv, a.lens, b);
+      const int n = pg_len(a.pv, a.lens[b]);
       int fit = rs.n;
       if (fit > cap - n) {
         pg_flag(a.pv, PG_BAD_LEN);
@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(PP_THREADS) k_paged_append(const PagedAppendAr
     place[0] = -1;
     if (b >= 0) {
       const RowSpan rs = pg_rows(a.pv, a.row_off, b, a.max_rows, a.n_rows);
-      const int n = pg_len(a.pv, a.lens, b), i = r - rs.first;
+      const int n = pg_len(a.pv, a.lens[b]), i = r - rs.first;
       if (i >= 0 && i < rs.n && n + i < cap) {
         const int id = pg_page(a.pv, b, n + i);
         if (id >= 0) {
@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(PE_THREADS) k_paged_select(const PagedEvictArg
   __shared__ unsigned found[3];                    // bin, count ahead of it, count in it
   pdl_begin();
   const int unit = blockIdx.x, b = unit / a.pv.hkv, cap = pg_capacity(a.pv), tid = threadIdx.x;
-  const int n = pg_len(a.pv, a.lens, b);
+  const int n = pg_len(a.pv, a.lens[b]);
   const long long base = (long long)unit * cap;
   int* moves = a.moves + (long long)unit * (1 + 2 * (long long)a.max_moves);
   if (unit % a.pv.hkv == 0 && tid == 0) a.lens_out[b] = min(n, a.budget);

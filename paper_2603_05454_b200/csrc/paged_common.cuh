@@ -21,9 +21,9 @@ __device__ __forceinline__ void pg_flag(const PagedView& pv, int bit) {
 }
 __device__ __forceinline__ int pg_capacity(const PagedView& pv) { return pv.max_pages * pv.page; }
 
-// Slots in use of sequence b, inside [0, capacity].
-__device__ __forceinline__ int pg_len(const PagedView& pv, const int* lens, int b) {
-  const int n = lens[b], cap = pg_capacity(pv);
+// Slots in use, n as the caller's array has it, inside [0, capacity].
+__device__ __forceinline__ int pg_len(const PagedView& pv, int n) {
+  const int cap = pg_capacity(pv);
   if (n < 0 || n > cap) {
     pg_flag(pv, PG_BAD_LEN);
     return n < 0 ? 0 : cap;

@@ -18,7 +18,7 @@ MHA, GQA, SMALL, ONE = (8, 8, 128), (28, 4, 128), (8, 4, 64), (1, 1, 64)
 def _cache(pool, max_rows=1, weights=False, n_rows=None, table=True):
     from paper_2603_05454_b200 import PagedKVCache
     c = PagedKVCache(pool.k, pool.v, pool.table if table else None, n_heads=pool.heads[0], max_rows=max_rows, weights=weights, n_rows=n_rows)
-    c.workspace.fill_(0xFF)                        # NaN bit patterns: no result depends on what nobody wrote
+    c.workspace[4096:].fill_(0xFF)                 # NaN bit patterns: no result depends on what nobody wrote
     return c
 
 
