@@ -112,7 +112,7 @@ def test_workspace_sizes():
     kv = _kv()
     plain = ws(C.byref(kv), 8, 6, 0)
     assert plain > 0 and plain % 256 == 0
-    assert ws(C.byref(kv), 8, 6, 1) >= plain + 6 * 8 * (64 + 2) * 4          # a score per row, head and slot
+    assert ws(C.byref(kv), 8, 6, 1) >= plain + 6 * 8 * 64 * 4                # a score per row, head and slot
     assert ws(C.byref(kv), 0, 6, 0) == 0 and ws(C.byref(kv), 8, -1, 0) == 0
     ev = B.lib.lsp_paged_evict_workspace
     assert ev(C.byref(kv), 32) >= 2 * 4 * (1 + 2 * 32) * 4                   # 32 of 64 slots move at most
