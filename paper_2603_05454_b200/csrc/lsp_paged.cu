@@ -131,6 +131,21 @@ cudaError_t launch_attention(const PagedAttnArgs& a0, int tiles, cudaStream_t st
   return launch_k(1, k_paged_weights, dim3(a.pv.batch * a.pv.hkv * key_blocks), dim3(PW_THREADS), (size_t)a.max_rows * a.group * 4, stream, a, key_blocks);
 }
 
+// The selection's launch: 1024 threads a CTA, a cluster of CTAs per unit while that fills no more than the SMs and leaves each CTA 4096 slots;
+// 256 threads where there are more units than SMs (several fit an SM) and a thread has at most 32 slots.
+cudaError_t launch_select(PagedEvictArgs& a, int units, int cap, int n_sm, cudaStream_t stream) {
+  const bool small = units > n_sm && cap <= 8192;
+  a.cluster = 1;
+  while (!small && a.cluster < 8 && 2 * a.cluster * units <= n_sm && cap / (2 * a.cluster) >= 2048) a.cluster *= 2;
+  a.slots = ((cap + 31) / 32 + a.cluster - 1) / a.cluster * 32;
+  a.in_smem = a.slots <= PE_KEYS ? 1 : 0;
+  const int threads = small ? 256 : 1024;
+  const size_t smem = (size_t)2 * threads * 4 + a.slots / 8 + (a.in_smem ? (size_t)a.slots * 4 : 0);
+  void (*kern)(PagedEvictArgs) = small ? k_paged_select<256> : k_paged_select<1024>;
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  return e != cudaSuccess ? e : launch_k(1, kern, dim3(units * a.cluster), dim3(threads), smem, stream, a.cluster, a);
+}
+
 }  // namespace
 
 extern "C" {
@@ -280,9 +295,10 @@ int lsp_paged_evict(const lsp_paged_kv* kv, const float* weights, const int32_t*
   a.head_bytes = kv->head_dim * a.esz;
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   const int units = kv->batch * kv->n_kv_heads;
-  const size_t smem = (size_t)PE_BINS * 4 + (size_t)(cap + 31) / 32 * 4;
-  cudaError_t ce = cudaFuncSetAttribute(k_paged_select, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (ce == cudaSuccess) ce = launch_k(1, k_paged_select, dim3(units), dim3(PE_THREADS), smem, st, a);
+  int dev = 0, n_sm = 0;
+  cudaError_t ce = cudaGetDevice(&dev);
+  if (ce == cudaSuccess) ce = cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev);
+  if (ce == cudaSuccess) ce = launch_select(a, units, (int)cap, n_sm, st);
   if (ce == cudaSuccess && a.max_moves > 0)
     ce = launch_k(1, k_paged_move, dim3(units, (a.max_moves + PM_WARPS * PM_PAIRS - 1) / (PM_WARPS * PM_PAIRS)), dim3(PM_WARPS * 32), 0, st, a);
   if (ce != cudaSuccess) return e.fail(LSP_ERR_CUDA, "%s: launch failed (%s)", who, cudaGetErrorString(ce));

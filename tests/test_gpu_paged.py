@@ -417,6 +417,27 @@ def test_evict_from_a_long_sequence(n, budget):
     _check_evict(pool, w, pos, budget, 5, 50)
 
 
+def test_evict_from_more_slots_than_are_kept_on_chip():
+    pool = U.Pool([400001], (1, 1, 64), BF, 64)
+    w, pos = _weights(pool, 17)
+    _check_evict(pool, w, pos, 150000, 5, 5000)
+
+
+@pytest.mark.parametrize("budget", [40, 75])
+def test_evict_of_many_heads(budget):
+    pool = U.Pool([70 + b % 9 for b in range(40)], (8, 8, 64), BF, 16)
+    w, pos = _weights(pool, 18)
+    _check_evict(pool, w, pos, budget, 3, 11)
+
+
+@pytest.mark.parametrize("values", [[1.0], [0.0, 2.0]])
+def test_ties_over_a_cluster(values):
+    pool = U.Pool([20000], (2, 2, 64), BF, 64)
+    _, pos = _weights(pool, 19)
+    w = torch.tensor(values)[torch.randint(len(values), (1, 2, pool.cap), generator=torch.Generator().manual_seed(3))].to(DEV)
+    _check_evict(pool, w, pos, 15000, 3, 11)
+
+
 def test_evict_without_positions_goes_by_slots():
     pool = U.Pool([300, 20], SMALL, BF, 16)
     w, _ = _weights(pool, 8)
