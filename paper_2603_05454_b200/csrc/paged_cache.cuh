@@ -118,6 +118,9 @@ __global__ void __launch_bounds__(PP_THREADS) k_paged_append(const PagedAppendAr
 // Each CTA of the cluster has a run of the slots, their keys in shared memory (read from global memory once); a digit's counts
 // are added over distributed shared memory.  Bound by the chain of passes: a digit costs a read of the keys from shared memory and four barriers.
 constexpr int PE_MAX_CAP = 1 << 20;     // slots of a sequence: a bitmap of 128 KB
+constexpr int PE_BITS = 11, PE_BINS = 1 << PE_BITS;      // a digit
+constexpr int PE_CLUSTER = 8;           // CTAs of a unit at most
+constexpr int PE_SLOTS = 128 * 1024;    // slots of a CTA at most (its bitmap and what goes with it: 48 KB)
 constexpr int PE_KEYS = 40 * 1024;      // slots of a CTA whose keys fit shared memory; beyond that a pass reads them again
 constexpr int PM_WARPS = 8;
 constexpr int PM_PAIRS = 4;             // pairs of a warp that are under way at once
@@ -143,46 +146,74 @@ __device__ __forceinline__ unsigned pe_key(float w) {
   return ~u;                                  // +inf: 0x007fffff
 }
 
-// n of this thread added up over the threads before it; all: over all of the block's.
+// x and y of this thread added up over the threads before it; all: over all of the block's.
 template <int THREADS>
-__device__ __forceinline__ int pe_sum_before(int n, int* warp_sums, int& all) {
+__device__ __forceinline__ int2 pe_sums_before(int2 v, int2* warp_sums, int2& all) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  int x = n;
+  auto scan = [&](int2 x) {
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, x, o);
-    if (lane >= o) x += y;
-  }
+    for (int o = 1; o < 32; o <<= 1) {
+      const int p = __shfl_up_sync(0xffffffffu, x.x, o), q = __shfl_up_sync(0xffffffffu, x.y, o);
+      if (lane >= o) {
+        x.x += p;
+        x.y += q;
+      }
+    }
+    return x;
+  };
+  const int2 x = scan(v);
   __syncthreads();
   if (lane == 31) warp_sums[w] = x;
   __syncthreads();
-  const int s = lane < THREADS / 32 ? warp_sums[lane] : 0;      // every warp adds the sums up for itself
-  int t = s;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, t, o);
-    if (lane >= o) t += y;
-  }
-  all = __shfl_sync(0xffffffffu, t, 31);
-  return x - n + __shfl_sync(0xffffffffu, t - s, w);
+  const int2 s = lane < THREADS / 32 ? warp_sums[lane] : make_int2(0, 0), t = scan(s);      // every warp adds the sums up for itself
+  all = make_int2(__shfl_sync(0xffffffffu, t.x, 31), __shfl_sync(0xffffffffu, t.y, 31));
+  return make_int2(x.x - v.x + __shfl_sync(0xffffffffu, t.x - s.x, w), x.y - v.y + __shfl_sync(0xffffffffu, t.y - s.y, w));
 }
 
+// x of this lane added up over the lanes before it.
+__device__ __forceinline__ int pe_warp_sum_before(int x) {
+  int y = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int p = __shfl_up_sync(0xffffffffu, y, o);
+    if ((int)(threadIdx.x & 31) >= o) y += p;
+  }
+  return y - x;
+}
+
+// Words of shared memory of another CTA of the cluster.
 __device__ __forceinline__ int ld_cluster_s32(uint32_t addr) {
   int v;
   asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
   return v;
 }
+__device__ __forceinline__ int2 ld_cluster_s32x2(uint32_t addr) {
+  int2 v;
+  asm volatile("ld.shared::cluster.v2.s32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint4 ld_cluster_u4(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
+// Shared memory of a selection, in words: counts, bitmap, holes and movers ahead of each of its words, keys.
+__host__ __device__ inline int pe_words(int slots, int in_smem) { return 2 * PE_BINS + slots / 32 * 3 + 4 + (in_smem ? slots : 0); }
 
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a) {
-  constexpr int BINS = 2 * THREADS, BITS = THREADS == 1024 ? 11 : THREADS == 512 ? 10 : 9;      // two bins a thread
-  static_assert(1 << BITS == BINS, "two bins a thread");
-  extern __shared__ unsigned pe_smem[];
-  unsigned* hist = pe_smem;                        // [BINS]
-  unsigned* bits = pe_smem + BINS;                 // [slots / 32] kept slots of this CTA
-  unsigned* keys = bits + a.slots / 32;            // [slots]
-  __shared__ int warp_sums[32], found[3], counts[2];
-  const int CL = a.cluster, rank = CL > 1 ? (int)cluster_ctarank() : 0, tid = threadIdx.x;
+  extern __shared__ __align__(16) unsigned pe_smem[];
+  unsigned* keys = pe_smem + 2 * PE_BINS;          // behind two sets of counts: [slots], if they are kept here
+  unsigned* bits = keys + (a.in_smem ? a.slots : 0);      // [slots / 32] kept slots of this CTA
+  int* holes_at = reinterpret_cast<int*>(bits + a.slots / 32);
+  int* movers_at = holes_at + a.slots / 32;
+  __shared__ int2 warp_sums[32];
+  __shared__ __align__(16) int found[4], shared_counts[4];
+  __shared__ unsigned warp_or[32];
+  __shared__ int groups_of[2][PE_BINS / 64];
+  int turn = 0;
+  const int CL = a.cluster, rank = CL > 1 ? (int)cluster_ctarank() : 0, tid = threadIdx.x, lane = tid & 31;
   auto barrier = [&]() { if (CL > 1) cluster_sync(); else __syncthreads(); };
   pdl_begin();
   const int unit = blockIdx.x / CL, b = unit / a.pv.hkv, cap = pg_capacity(a.pv);
@@ -194,64 +225,96 @@ __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a
   const int run = ((n + 31) / 32 + CL - 1) / CL * 32, s0 = min(n, rank * run), ns = min(n, s0 + run) - s0;
   const float* weights = a.weights + base + s0;
   const int* pos = a.pos ? a.pos + base + s0 : nullptr;
+  float* weights_out = a.weights_out + base + s0;
+  int* pos_out = a.pos_out ? a.pos_out + base + s0 : nullptr;
+  auto pos_of = [&](int j) { return pos ? pos[j] : s0 + j; };
   if (n <= a.budget) {
     if (rank == 0 && tid == 0) moves[0] = 0;
     for (int j = tid; j < ns; j += THREADS) {
-      a.weights_out[base + s0 + j] = weights[j];
-      if (a.pos_out) a.pos_out[base + s0 + j] = pos ? pos[j] : s0 + j;
+      weights_out[j] = weights[j];
+      if (pos_out) pos_out[j] = pos_of(j);
     }
     return;
   }
   const int seen = a.seen ? a.seen[b] : n;
-  auto pos_of = [&](int j) { return pos ? pos[j] : s0 + j; };
-  auto read_key = [&](int j) {
-    const int p = pos_of(j);
-    const float w = weights[j];
-    return (p < a.n_sink || p >= seen - a.n_recent) ? 0u : pe_key(w);
-  };
+  auto key_of = [&](int p, float w) { return (p < a.n_sink || p >= seen - a.n_recent) ? 0u : pe_key(w); };
+  unsigned any = 0;                                // bits that some position has
   if (a.in_smem)
-    for (int j = tid; j < ns; j += THREADS) keys[j] = read_key(j);
-  auto key = [&](int j) { return a.in_smem ? keys[j] : read_key(j); };
-  // The need-th smallest 32-bit value that `get` gives for the slots it says true of: the value, how many are below it, how many equal it.
-  // (Where all values of a prefix are wanted, the rest of the digits are: value = the largest with that prefix.)
-  auto select = [&](auto get, int need, unsigned& value, int& below, int& equal) {
-    unsigned prefix = 0, mask = 0;
+#pragma unroll 8
+    for (int j = tid; j < ns; j += THREADS) {
+      const int p = pos_of(j);
+      keys[j] = key_of(p, weights[j]);
+      any |= (unsigned)p;
+    }
+  else
+    for (int j = tid; j < ns; j += THREADS) any |= (unsigned)pos_of(j);
+  any = __reduce_or_sync(0xffffffffu, any);
+  if (lane == 0) warp_or[tid >> 5] = any;
+  auto key = [&](int j) { return a.in_smem ? keys[j] : key_of(pos_of(j), weights[j]); };
+  // The need-th smallest value of at most `width` bits that `get` gives for the slots it says true of: the value, how many are below it, how many
+  // equal it.  (Where all values of a prefix are wanted, the rest of the digits are: value = the largest with that prefix.)
+  auto select = [&](auto get, int width, int need, unsigned& value, int& below, int& equal) {
+    unsigned prefix = 0, mask = width == 32 ? 0u : ~0u << width;
     below = 0;
 #pragma unroll 1
-    for (int shift = 32 - BITS;; shift = max(0, shift - BITS)) {
+    for (int shift = max(0, width - PE_BITS);; shift = max(0, shift - PE_BITS)) {
       const unsigned digit = ~mask >> shift;         // mask of the digit's bits (the last one may be shorter)
-      hist[tid] = 0;
-      hist[tid + THREADS] = 0;
+      turn ^= 1;                                     // two sets of counts in turn: another CTA may still be reading the last pass's
+      unsigned* hist = pe_smem + turn * PE_BINS;
+      int* groups = groups_of[turn];
+#pragma unroll
+      for (int i = tid; i < PE_BINS / 4; i += THREADS) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
       __syncthreads();
 #pragma unroll 4
       for (int j = tid; j < ns; j += THREADS) {
         unsigned k;
         if (get(j, k) && (k & mask) == prefix) atomicAdd(&hist[(k >> shift) & digit], 1u);
       }
+      __syncthreads();
+      // counts of 64 bins each, a warp a group; the first warp finds the group in which the need-th lies, then the bin
+      for (int g = tid >> 5; g < PE_BINS / 64; g += THREADS / 32) {
+        const uint2 x = reinterpret_cast<const uint2*>(hist)[g * 32 + lane];
+        const unsigned s = __reduce_add_sync(0xffffffffu, x.x + x.y);
+        if (lane == 0) groups[g] = s;
+      }
       barrier();
-      int h0 = 0, h1 = 0;
-      if (CL == 1) {
-        const uint2 h = reinterpret_cast<const uint2*>(hist)[tid];
-        h0 = h.x;
-        h1 = h.y;
-      } else {
-        const uint32_t mine = smem_u32(hist + 2 * tid);
-        for (int r = 0; r < CL; ++r) {
-          const uint32_t at = cluster_map(mine, r);
-          h0 += ld_cluster_s32(at);
-          h1 += ld_cluster_s32(at + 4);
+      if (tid < 32) {
+        const int want = need - below;               // rank, from 1, among what is left
+        int x = CL == 1 ? groups[lane] : 0;
+        if (CL > 1) {
+          int y[PE_CLUSTER];
+#pragma unroll
+          for (int r = 0; r < PE_CLUSTER; ++r) y[r] = r < CL ? ld_cluster_s32(cluster_map(smem_u32(groups + lane), r)) : 0;
+#pragma unroll
+          for (int r = 0; r < PE_CLUSTER; ++r) x += y[r];
+        }
+        int up = pe_warp_sum_before(x) + x;
+        const int g = __ffs(__ballot_sync(0xffffffffu, want <= up)) - 1, base_g = __shfl_sync(0xffffffffu, up - x, g);
+        int2 h = make_int2(0, 0);
+        const unsigned* mine = hist + g * 64 + lane * 2;
+        if (CL == 1) {
+          h = *reinterpret_cast<const int2*>(mine);
+        } else {
+          int2 y[PE_CLUSTER];
+#pragma unroll
+          for (int r = 0; r < PE_CLUSTER; ++r) y[r] = r < CL ? ld_cluster_s32x2(cluster_map(smem_u32(mine), r)) : make_int2(0, 0);
+#pragma unroll
+          for (int r = 0; r < PE_CLUSTER; ++r) {
+            h.x += y[r].x;
+            h.y += y[r].y;
+          }
+        }
+        up = base_g + pe_warp_sum_before(h.x + h.y) + h.x + h.y;
+        const int l = __ffs(__ballot_sync(0xffffffffu, want <= up)) - 1;
+        if (lane == l) {
+          const int before = up - h.x - h.y;
+          const bool second = want > before + h.x;
+          found[0] = g * 64 + lane * 2 + (second ? 1 : 0);
+          found[1] = second ? before + h.x : before;
+          found[2] = second ? h.y : h.x;
         }
       }
-      int all;
-      const int before = pe_sum_before<THREADS>(h0 + h1, warp_sums, all);
-      const int want = need - below;                 // rank, from 1, among what is left
-      if (before < want && want <= before + h0 + h1) {
-        const bool second = want > before + h0;
-        found[0] = 2 * tid + (second ? 1 : 0);
-        found[1] = before + (second ? h0 : 0);
-        found[2] = second ? h1 : h0;
-      }
-      barrier();                                     // (and the others have read this CTA's counts)
+      __syncthreads();
       prefix |= (unsigned)found[0] << shift;
       mask |= digit << shift;
       below += found[1];
@@ -260,115 +323,171 @@ __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a
     }
     value = prefix | ~mask;
   };
-  unsigned key_at, pos_at = 0xffffffffu, slot_at = 0xffffffffu;
+  unsigned key_at, pos_at = 0xffffffffu, slot_at = 0xffffffffu, flip = 0;
   int below, equal;
-  __syncthreads();
-  select([&](int j, unsigned& k) { k = key(j); return true; }, a.budget, key_at, below, equal);
-  if (below + equal > a.budget) {                   // ties of the weight: the lower positions
+  select([&](int j, unsigned& k) { k = key(j); return true; }, 32, a.budget, key_at, below, equal);
+  const bool ties = below + equal > a.budget;
+  if (ties) {                                       // ties of the weight: the lower positions
+    unsigned bits_used = 0;
+    for (int i = 0; i < THREADS / 32; ++i) bits_used |= warp_or[i];
+    if (CL > 1) {
+      if (tid == 0) shared_counts[2] = (int)bits_used;
+      cluster_sync();
+      for (int r = 0; r < CL; ++r) bits_used |= ld_cluster_u4(cluster_map(smem_u32(shared_counts), r)).z;
+    }
+    flip = bits_used & 0x80000000u;                 // (negative positions are lower than others)
     int need = a.budget - below;
-    select([&](int j, unsigned& k) { const bool tie = key(j) == key_at; k = tie ? (unsigned)pos_of(j) ^ 0x80000000u : 0u; return tie; }, need, pos_at, below, equal);
+    select([&](int j, unsigned& k) { const bool tie = key(j) == key_at; k = tie ? (unsigned)pos_of(j) ^ flip : 0u; return tie; }, 32 - __clz(bits_used | 1u), need,
+           pos_at, below, equal);
     if (below + equal > need) {                     // the same position twice: the lower slots
       need -= below;
-      select([&](int j, unsigned& k) { k = (unsigned)(s0 + j); return key(j) == key_at && ((unsigned)pos_of(j) ^ 0x80000000u) == pos_at; }, need, slot_at, below, equal);
+      select([&](int j, unsigned& k) { k = (unsigned)(s0 + j); return key(j) == key_at && ((unsigned)pos_of(j) ^ flip) == pos_at; }, 32 - __clz(n), need, slot_at, below,
+             equal);
     }
   }
-  const bool by_pos = pos_at != 0xffffffffu || slot_at != 0xffffffffu;
   auto kept = [&](int j) {
     const unsigned k = key(j);
-    if (k != key_at || !by_pos) return k <= key_at;
-    const unsigned p = (unsigned)pos_of(j) ^ 0x80000000u;
+    if (k != key_at || !ties) return k <= key_at;
+    const unsigned p = (unsigned)pos_of(j) ^ flip;
     return p < pos_at || (p == pos_at && (unsigned)(s0 + j) <= slot_at);
   };
   // bitmap of this CTA's run, a word a warp and turn
   const int words = (ns + 31) / 32;
   for (int j0 = tid & ~31; j0 < words * 32; j0 += THREADS) {
-    const int j = j0 + (tid & 31);
+    const int j = j0 + lane;
     const unsigned m = __ballot_sync(0xffffffffu, j < ns && kept(j));
-    if ((tid & 31) == 0) bits[j0 >> 5] = m;
+    if (lane == 0) bits[j0 >> 5] = m;
   }
   __syncthreads();
-  // freed slots ahead of the budget and kept ones behind it, in slot order; a thread takes a run of words
+  // freed slots ahead of the budget and kept ones behind it: how many lie ahead of each word; a thread takes a run of words
+  auto ahead = [&](int w) { const int r = a.budget - (s0 + w * 32); return r >= 32 ? 0xffffffffu : r <= 0 ? 0u : (1u << r) - 1; };   // bits of slots < budget
   const int per = (words + THREADS - 1) / THREADS;
   const int w0 = min(words, tid * per), w1 = min(words, w0 + per);
-  auto ahead = [&](int w) { const int r = a.budget - (s0 + w * 32); return r >= 32 ? 0xffffffffu : r <= 0 ? 0u : (1u << r) - 1; };   // bits of slots < budget
-  int holes = 0, movers = 0;
+  int2 count = make_int2(0, 0), all;
   for (int w = w0; w < w1; ++w) {
-    holes += __popc(~bits[w] & ahead(w));
-    movers += __popc(bits[w] & ~ahead(w));
+    count.x += __popc(~bits[w] & ahead(w));
+    count.y += __popc(bits[w] & ~ahead(w));
   }
-  int all_holes, all_movers;
-  int ih = pe_sum_before<THREADS>(holes, warp_sums, all_holes);
-  int im = pe_sum_before<THREADS>(movers, warp_sums, all_movers);
+  int2 at = pe_sums_before<THREADS>(count, warp_sums, all);
+  int movers = all.y;
   if (CL > 1) {
     if (tid == 0) {
-      counts[0] = all_holes;
-      counts[1] = all_movers;
+      shared_counts[0] = all.x;
+      shared_counts[1] = all.y;
     }
     cluster_sync();
-    all_movers = 0;
-    for (int r = 0; r < CL; ++r) {
-      const uint32_t at = cluster_map(smem_u32(counts), r);
-      const int h = ld_cluster_s32(at), m = ld_cluster_s32(at + 4);
-      ih += r < rank ? h : 0;
-      im += r < rank ? m : 0;
-      all_movers += m;
-    }
+    uint4 x[PE_CLUSTER];
+#pragma unroll
+    for (int r = 0; r < PE_CLUSTER; ++r)
+      if (r < CL) x[r] = ld_cluster_u4(cluster_map(smem_u32(shared_counts), r));
+    movers = 0;
+#pragma unroll
+    for (int r = 0; r < PE_CLUSTER; ++r)
+      if (r < CL) {
+        at.x += r < rank ? (int)x[r].x : 0;
+        at.y += r < rank ? (int)x[r].y : 0;
+        movers += (int)x[r].y;
+      }
+    // Nobody leaves while another reads its counts; that orders no memory, and an arrival with release would wait for the stores below.
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   }
-  if (rank == 0 && tid == 0) moves[0] = all_movers;
+  for (int w = w0; w < w1; ++w) {
+    holes_at[w] = at.x;
+    movers_at[w] = at.y;
+    at.x += __popc(~bits[w] & ahead(w));
+    at.y += __popc(bits[w] & ~ahead(w));
+  }
+  __syncthreads();
+  if (rank == 0 && tid == 0) moves[0] = movers;
   int* src = moves + 1;
   int* dst = src + a.max_moves;
-  for (int w = w0; w < w1; ++w) {
-    for (unsigned m = ~bits[w] & ahead(w); m; m &= m - 1) dst[ih++] = s0 + w * 32 + __ffs(m) - 1;
-    for (unsigned m = bits[w] & ~ahead(w); m; m &= m - 1) src[im++] = s0 + w * 32 + __ffs(m) - 1;
-  }
-  for (int j = tid; j < min(ns, a.budget - s0); j += THREADS)
-    if ((bits[j >> 5] >> (j & 31)) & 1) {
-      a.weights_out[base + s0 + j] = weights[j];
-      if (a.pos_out) a.pos_out[base + s0 + j] = pos_of(j);
+  const unsigned lower = (1u << lane) - 1;
+  constexpr int AT_ONCE = 4;                         // words of a warp whose weights and positions are under way
+  for (int w4 = tid >> 5; w4 < words; w4 += AT_ONCE * (THREADS / 32)) {
+    float weight[AT_ONCE];
+    int p[AT_ONCE];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int w = w4 + i * (THREADS / 32);
+      const bool stays = w < words && ((bits[w] & ahead(w)) >> lane & 1);
+      weight[i] = stays ? weights[w * 32 + lane] : 0.f;
+      p[i] = stays && pos_out ? pos_of(w * 32 + lane) : 0;
     }
-  if (CL > 1) cluster_sync();                        // nobody leaves while another reads its counts
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int w = w4 + i * (THREADS / 32);
+      if (w >= words) break;
+      const unsigned m = bits[w], front = ahead(w);
+      const int j = w * 32 + lane;
+      const bool is_kept = (m >> lane) & 1, is_front = (front >> lane) & 1;
+      if (is_front && is_kept) {                     // stays
+        weights_out[j] = weight[i];
+        if (pos_out) pos_out[j] = p[i];
+      }
+      if (is_front && !is_kept) dst[holes_at[w] + __popc(~m & front & lower)] = s0 + j;
+      if (!is_front && is_kept) src[movers_at[w] + __popc(m & ~front & lower)] = s0 + j;
+    }
+  }
+  if (CL > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
 }
 
 // What moves: weight, position and rows.  A warp takes PM_PAIRS pairs of slots at a time; the K row in the first half of the lanes, the V row in
-// the second (rows of 512 bytes in two turns).
+// the second (rows of 512 bytes in two turns).  A turn's rows are under way while the next one's pages, and the slots of the one behind it,
+// are looked up: without that the chain of the four reads is what a warp waits for.
 __global__ void __launch_bounds__(PM_WARPS * 32) k_paged_move(const PagedEvictArgs a) {
   pdl_begin();
   const int unit = blockIdx.x, b = unit / a.pv.hkv, kvh = unit % a.pv.hkv, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int* moves = a.moves + (long long)unit * (1 + 2 * (long long)a.max_moves);
-  const int n = moves[0];
-  const int i0 = (blockIdx.y * PM_WARPS + w) * PM_PAIRS;
+  const int* list = moves + 1 + (lane < PM_PAIRS ? 0 : a.max_moves);      // lanes 0 .. 3: sources, lanes 4 .. 7: targets
+  const int n = moves[0], step = gridDim.y * PM_WARPS * PM_PAIRS;
+  int i0 = (blockIdx.y * PM_WARPS + w) * PM_PAIRS;
   if (i0 >= n) return;
-  // lanes 0 .. 3: source of a pair, lanes 4 .. 7: its target
-  long long off = -1;
-  int j = 0;
-  const bool mine = lane < 2 * PM_PAIRS && i0 + lane % PM_PAIRS < n;
-  if (mine) {
-    j = moves[1 + (lane < PM_PAIRS ? 0 : a.max_moves) + i0 + lane % PM_PAIRS];
-    const int id = pg_page(a.pv, b, j);
-    if (id >= 0) off = ((long long)id * a.pv.page_stride + (long long)(j % a.pv.page) * a.pv.row_stride + (long long)kvh * a.pv.head_stride) * a.esz;
-  }
-  const int target = __shfl_down_sync(0xffffffffu, j, PM_PAIRS);
-  if (mine && lane < PM_PAIRS) {
-    const long long base = (long long)unit * pg_capacity(a.pv);
-    a.weights_out[base + target] = a.weights[base + j];
-    if (a.pos_out) a.pos_out[base + target] = a.pos ? a.pos[base + j] : j;
-  }
-  long long from[PM_PAIRS], to[PM_PAIRS];
-#pragma unroll
-  for (int i = 0; i < PM_PAIRS; ++i) {
-    from[i] = __shfl_sync(0xffffffffu, off, i);
-    to[i] = __shfl_sync(0xffffffffu, off, PM_PAIRS + i);
-    if (from[i] < 0) to[i] = -1;
-  }
+  const long long base = (long long)unit * pg_capacity(a.pv);
+  auto slot = [&](int i) { i += lane % PM_PAIRS; return lane < 2 * PM_PAIRS && i < n ? list[i] : -1; };
+  auto offset = [&](int j) -> long long {
+    const int id = j >= 0 ? pg_page(a.pv, b, j) : -1;
+    return id < 0 ? -1 : ((long long)id * a.pv.page_stride + (long long)(j % a.pv.page) * a.pv.row_stride + (long long)kvh * a.pv.head_stride) * a.esz;
+  };
+  int j = slot(i0), j2 = slot(i0 + step);
+  long long off = offset(j);
   char* pool = lane < 16 ? a.pv.k : a.pv.v;
-  for (int c = (lane & 15) * 16; c < a.head_bytes; c += 256) {
+  for (; i0 < n; i0 += step) {
+    const int target = __shfl_down_sync(0xffffffffu, j, PM_PAIRS);
+    long long from[PM_PAIRS], to[PM_PAIRS];
+#pragma unroll
+    for (int i = 0; i < PM_PAIRS; ++i) {
+      from[i] = __shfl_sync(0xffffffffu, off, i);
+      to[i] = __shfl_sync(0xffffffffu, off, PM_PAIRS + i);
+      if (from[i] < 0) to[i] = -1;
+    }
+    const int c0 = (lane & 15) * 16;
     uint4 x[PM_PAIRS];
 #pragma unroll
     for (int i = 0; i < PM_PAIRS; ++i)
-      if (to[i] >= 0) x[i] = *reinterpret_cast<const uint4*>(pool + from[i] + c);
+      if (to[i] >= 0 && c0 < a.head_bytes) x[i] = *reinterpret_cast<const uint4*>(pool + from[i] + c0);
+    const bool mine = lane < PM_PAIRS && j >= 0;
+    const float weight = mine ? a.weights[base + j] : 0.f;
+    const int p = mine && a.pos ? a.pos[base + j] : j;
+    const int j3 = slot(i0 + 2 * step);
+    const long long off2 = offset(j2);
 #pragma unroll
     for (int i = 0; i < PM_PAIRS; ++i)
-      if (to[i] >= 0) *reinterpret_cast<uint4*>(pool + to[i] + c) = x[i];
+      if (to[i] >= 0 && c0 < a.head_bytes) *reinterpret_cast<uint4*>(pool + to[i] + c0) = x[i];
+    if (c0 + 256 < a.head_bytes) {
+#pragma unroll
+      for (int i = 0; i < PM_PAIRS; ++i)
+        if (to[i] >= 0) x[i] = *reinterpret_cast<const uint4*>(pool + from[i] + c0 + 256);
+#pragma unroll
+      for (int i = 0; i < PM_PAIRS; ++i)
+        if (to[i] >= 0) *reinterpret_cast<uint4*>(pool + to[i] + c0 + 256) = x[i];
+    }
+    if (mine) {
+      a.weights_out[base + target] = weight;
+      if (a.pos_out) a.pos_out[base + target] = p;
+    }
+    j = j2;
+    j2 = j3;
+    off = off2;
   }
 }
 
