@@ -432,10 +432,10 @@ class PagedKVCache:
 
     def _rows(self, name, t, width):
         """Address, count and distance of packed rows [n_rows, width]."""
-        if t.dtype is not self.dtype or t.dim() != 2 or t.shape[1] != width or t.get_device() != self._index or t.stride(1) != 1:
+        shape, stride = t.shape, t.stride()
+        if t.dtype is not self.dtype or len(shape) != 2 or shape[1] != width or stride[1] != 1 or t.get_device() != self._index:
             raise ValueError(f"{name} must be a {self.dtype} tensor of shape [rows, {width}] on {self.device}, elements of a row contiguous")
-        n = t.shape[0]
-        return t.data_ptr(), n, t.stride(0) if n > 1 else max(t.stride(0), width)
+        return t.data_ptr(), shape[0], stride[0] if shape[0] > 1 else max(stride[0], width)
 
     def _row_off(self, row_off, n_rows, max_rows):
         """Address of the offsets and the bound of a sequence's rows."""

@@ -71,15 +71,15 @@ bool overlap(const void* a, const void* b, size_t bytes_a, size_t bytes_b) {
 }
 
 constexpr size_t kCounters = 4096;        // the first bytes of a workspace: arrival counters, 0 between calls
-static_assert(PA_MAX_CTAS * 4 <= kCounters, "a counter per CTA");
+static_assert(pa_max_ctas(64) * 4 <= kCounters && pa_max_ctas(128) * 4 <= kCounters, "a counter per CTA");
 
 struct AttnLayout { size_t part_o, part_ml, row_lse, scores, total; };
 AttnLayout attn_layout(const lsp_paged_kv* kv, int n_heads, int n_rows, int with_weights) {
   AttnLayout L;
   size_t at = kCounters;
   auto take = [&](size_t bytes) { const size_t o = at; at += align256(bytes); return o; };
-  L.part_o = take((size_t)2 * PA_MAX_CTAS * PA_ROWS * kv->head_dim * 4);
-  L.part_ml = take((size_t)2 * PA_MAX_CTAS * PA_ROWS * 8);
+  L.part_o = take((size_t)2 * pa_max_ctas(kv->head_dim) * PA_ROWS * kv->head_dim * 4);
+  L.part_ml = take((size_t)2 * pa_max_ctas(kv->head_dim) * PA_ROWS * 8);
   L.row_lse = take(with_weights ? (size_t)n_rows * n_heads * 4 : 0);
   L.scores = take(with_weights ? (size_t)n_rows * n_heads * kv->max_pages * kv->page_size * 4 : 0);
   L.total = at;
@@ -97,17 +97,18 @@ cudaError_t launch_attention(const PagedAttnArgs& a0, int tiles, cudaStream_t st
   using S = PaSmem<T, DH>;
   void (*kern)(PagedAttnArgs) = nullptr;
   a.q_rows = std::min(PA_ROWS, a.max_rows * a.group);
+  const bool a16 = a.pv.page % 16 == 0;
   if constexpr (sizeof(T) == 2) {
-    kern = k_paged_attn_mma<DH>;
+    kern = a16 ? k_paged_attn_mma<DH, true> : k_paged_attn_mma<DH, false>;
   } else {
-    kern = a.q_rows == 1 ? k_paged_attn_simt<DH, 1> : a.q_rows == 2 ? k_paged_attn_simt<DH, 2> : a.q_rows <= 4 ? k_paged_attn_simt<DH, 4>
-         : a.q_rows <= 8 ? k_paged_attn_simt<DH, 8> : k_paged_attn_simt<DH, 16>;
+    // (pages of other sizes: every slot's page is looked up, by the one kernel for any number of rows)
+    kern = !a16 ? k_paged_attn_simt<DH, 16, false> : a.q_rows == 1 ? k_paged_attn_simt<DH, 1, true> : a.q_rows == 2 ? k_paged_attn_simt<DH, 2, true>
+         : a.q_rows <= 4 ? k_paged_attn_simt<DH, 4, true> : a.q_rows <= 8 ? k_paged_attn_simt<DH, 8, true> : k_paged_attn_simt<DH, 16, true>;
   }
-  // Two CTAs an SM where their shared memory allows it; as many rows added at a time as are left room for.
+  // As many CTAs an SM as its registers hold, unless their shared memory forbids; as many rows added at a time as there is room for.
   constexpr int kStatic = 128, kSm = 228 * 1024, kCta = 227 * 1024 - kStatic, kOwn = 1024 + kStatic;
-  constexpr int per_sm = 2 * (S::RINGS + kOwn) <= kSm ? 2 : 1;
   int n_per_sm = 0, smem = 0;
-  for (int want = per_sm; want >= 1 && !n_per_sm; --want)
+  for (int want = pa_ctas_sm(DH, sizeof(T)); want >= 1 && !n_per_sm; --want)
     for (int rows = 4; rows >= 1 && !n_per_sm; rows /= 2) {
       smem = S::total(a.q_rows, rows, a.pv.batch);
       if (smem <= kCta && want * (smem + kOwn) <= kSm) {
@@ -124,7 +125,7 @@ cudaError_t launch_attention(const PagedAttnArgs& a0, int tiles, cudaStream_t st
   if (e != cudaSuccess) return e;
   const long long cap = (long long)a.pv.max_pages * a.pv.page;
   const long long most = ((cap + PA_CHUNK - 1) / PA_CHUNK + PA_UNIT_COST) * a.pv.batch * a.pv.hkv * tiles;       // numbers to deal, if every sequence were full
-  a.n_cta = (int)std::min<long long>(most, std::min(n_per_sm * n_sm, PA_MAX_CTAS));
+  a.n_cta = (int)std::min<long long>(most, std::min(n_per_sm * n_sm, pa_max_ctas(DH)));
   e = launch_k(1, kern, dim3(a.n_cta), dim3(PA_THREADS), (size_t)smem, stream, a);
   if (e != cudaSuccess || !a.scores) return e;
   const int key_blocks = (int)((cap + PW_KEYS - 1) / PW_KEYS);

@@ -26,7 +26,9 @@ constexpr int PA_WARPS = 4;
 constexpr int PA_THREADS = PA_WARPS * 32;
 constexpr int PA_ROWS = 16;             // (row, head) pairs of a unit
 constexpr int PA_MAX_BATCH = 1024;
-constexpr int PA_MAX_CTAS = 512;
+// CTAs of a launch at most (workspaces are sized by it), and on an SM: those that 64 warps' registers allow, so that 128 KB are in flight
+__host__ __device__ constexpr int pa_max_ctas(int dh) { return dh == 64 ? 1024 : 512; }
+__host__ __device__ constexpr int pa_ctas_sm(int dh, int esz) { return dh == 64 && esz == 2 ? 4 : dh == 128 && esz == 4 ? 1 : 2; }
 constexpr int PA_UNIT_COST = 2;         // what a unit costs besides its chunks, in chunks (queries, adding the warps' parts)
 constexpr int PW_THREADS = 256;
 constexpr int PW_KEYS = 1024;           // slots of a weights block
@@ -54,7 +56,8 @@ struct PagedAttnArgs {
 template <typename T, int DH>
 struct PaSmem {
   static constexpr int STAGE = 2 * 16 * DH * (int)sizeof(T);          // 16 rows of K, 16 of V
-  static constexpr int STAGES = STAGE > 8192 && DH == 128 ? 2 : 3;    // (fp32 rows of 512 bytes: 64 KB in flight with two)
+  // Two, 128 KB in flight an SM: 16 sequences of 12000 slots of 32 heads take 353 us, with three 376, with six 429 (one CTA an SM).
+  static constexpr int STAGES = 2;
   // Tiles of queries: those of as many units as chunks are asked for ahead, the next one's, and where the queries are not copied to registers at
   // once the present one's (a warp may still be in it when another has reached the next).
   static constexpr int Q_TILES = sizeof(T) == 4 ? STAGES + 1 : STAGES;
@@ -114,7 +117,7 @@ struct PaDeal {
     }
   }
   __device__ __forceinline__ int run(int i) const { return i * q + i * r / n; }
-  // the CTA whose run holds number c (the estimate is off by one at most: 2^-24 of at most PA_MAX_CTAS, and the runs' rounding)
+  // the CTA whose run holds number c (the estimate is off by one at most: 2^-24 of at most 1024, and the runs' rounding)
   __device__ __forceinline__ int owner(int c) const {
     int i = min(n - 1, (int)((float)c / (float)total * (float)n));
     while (run(i) > c) --i;
@@ -167,6 +170,10 @@ __device__ __forceinline__ bool pa_row(const PagedAttnArgs& a, const RowSpan& rs
   return true;
 }
 
+__device__ __forceinline__ void cp_async16_all(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
 // Byte offset of 16-byte chunk c of row r in a [16][DH] tile: chunks are exchanged within groups of eight by the row, so that eight
 // rows' chunks c lie in different banks.
 template <typename T, int DH>
@@ -181,30 +188,36 @@ __device__ __forceinline__ int pa_q_at(int r, int c) {
 }
 
 // One warp's loads: the rows of its 16 slots of a chunk, K then V, into one stage of its ring; and its part of the queries of a unit
-// that begins with the chunk.
-template <typename T, int DH>
+// that begins with the chunk.  A16: a page holds a multiple of 16 slots, so the 16 lie in one page, one behind the other; else every slot's page is
+// looked up.  (The 16 look-ups and 64-bit offsets took half of the kernel's instructions, and instructions, not bytes, were its time.)
+template <typename T, int DH, bool A16>
 struct PaLoader {
   static constexpr int CPR = DH * (int)sizeof(T) / 16;      // 16-byte chunks of a row
+  static constexpr int RPI = 32 / CPR;                      // rows of an instruction
+  static constexpr int WINDOW = A16 ? 32 : 2;               // chunks whose pages a lane's ids cover
   const PagedAttnArgs& a;
   const int* pre;
   int hi, w, lane;
   PaPlace p;
   bool first;                   // the next chunk is the run's first of its unit
   int tile;                     // of the unit that comes next
-  // page ids of this warp's slots: lanes 0 to 15 those of chunk `base`, 16 to 31 of the one behind it; the same two chunks on, under way
-  int base, ids, ids2;
+  // Pages ahead, and rows in the page: A16: lane i those of the warp's slots of chunk base + i; else lanes 0 to 15 those of the slots of
+  // chunk `base`, 16 to 31 of the one behind it.  The second ones, a window on, are under way.
+  int base, id, rem, id2, rem2;
   __device__ __forceinline__ PaLoader(const PagedAttnArgs& a_, const int* pre_, int hi_, const PaPlace& p_)
       : a(a_), pre(pre_), hi(hi_), w(threadIdx.x >> 5), lane(threadIdx.x & 31), p(p_), first(true), tile(0) {
     begin();
   }
-  __device__ __forceinline__ int ask(int chunk) const {
-    const int j = (chunk + (lane >> 4)) * PA_CHUNK + w * 16 + (lane & 15);
-    return j < p.len ? pg_page(a.pv, p.b, j) : -1;
+  __device__ __forceinline__ void ask(int chunk, int& page, int& row) const {
+    const int j = A16 ? (chunk + lane) * PA_CHUNK + w * 16 : (chunk + (lane >> 4)) * PA_CHUNK + w * 16 + (lane & 15);
+    const int end = A16 ? min(p.len, (p.chunk + p.left) * PA_CHUNK) : p.len;      // (no pages of chunks that are another CTA's)
+    page = j < end ? pg_page(a.pv, p.b, j) : -1;
+    row = j % a.pv.page;
   }
   __device__ __forceinline__ void begin() {
     base = p.chunk;
-    ids = ask(base);
-    ids2 = ask(base + 2);
+    ask(base, id, rem);
+    ask(base + WINDOW, id2, rem2);
   }
   // Returns a mask of the rows that are real slots.
   __device__ __forceinline__ unsigned issue(char* stage, char* q_tiles) {
@@ -215,34 +228,65 @@ struct PaLoader {
         char* q_tile = q_tiles + tile * PaSmem<T, DH>::q_tile(a.q_rows);
         if (++tile == PaSmem<T, DH>::Q_TILES) tile = 0;
         const int pieces = min(PA_ROWS, rs.n * a.group - p.rt * PA_ROWS) * CPR;
+#pragma unroll 1
         for (int i = threadIdx.x; i < pieces; i += PA_THREADS) {
           int row, head;
           pa_row(a, rs, p, i / CPR, row, head);
           cp_async16(smem_u32(q_tile + pa_q_at<T, DH>(i / CPR, i % CPR)), (const T*)a.q + (long long)row * a.ldq + head * DH + (i % CPR) * (16 / (int)sizeof(T)), true);
         }
       }
-      const int id = __shfl_sync(0xffffffffu, ids, (p.chunk - base) * 16 + (lane & 15));
-      const int j = p.chunk * PA_CHUNK + w * 16 + (lane & 15);
-      live = __ballot_sync(0xffffffffu, id >= 0) & 0xffffu;
-      const long long off = id < 0 ? 0 : (long long)id * a.pv.page_stride + (long long)(j % a.pv.page) * a.pv.row_stride + (long long)p.kvh * a.pv.head_stride;
+      // this lane's piece of row (lane / CPR) of the tile; the rows an instruction further on: exchanged chunks differ in the row's low bits
+      const int r0 = lane / CPR, ch = lane % CPR;
       const uint32_t ks = smem_u32(stage), vs = ks + 16 * DH * (int)sizeof(T);
+      const uint32_t at = r0 * DH * (int)sizeof(T) + ((ch ^ r0) << 4);
+      auto dst = [&](int i) { return i * RPI * DH * (int)sizeof(T) + (at ^ (((i * RPI) & 7) << 4)); };
+      if constexpr (A16) {
+        const int from = p.chunk - base, page = __shfl_sync(0xffffffffu, id, from), row = __shfl_sync(0xffffffffu, rem, from);
+        const int n = page < 0 ? 0 : min(16, p.len - (p.chunk * PA_CHUNK + w * 16));
+        live = n >= 16 ? 0xffffu : n <= 0 ? 0u : (1u << n) - 1;
+        const long long step = a.pv.row_stride * RPI * (int)sizeof(T);
+        const long long off = n <= 0 ? 0 : ((long long)page * a.pv.page_stride + (long long)(row + r0) * a.pv.row_stride + (long long)p.kvh * a.pv.head_stride) * (int)sizeof(T) + ch * 16;
+        const char *k = a.pv.k + off, *v = a.pv.v + off;
+        if (n >= 16) {
 #pragma unroll
-      for (int i = 0; i < 16 * CPR / 32; ++i) {
-        const int r = (i * 32 + lane) / CPR, ch = (i * 32 + lane) % CPR;
-        const long long o = __shfl_sync(0xffffffffu, off, r) * (int)sizeof(T) + ch * 16;
-        const bool v = (live >> r) & 1;
-        const int d = pa_at<T, DH>(r, ch);
-        cp_async16(ks + d, a.pv.k + (v ? o : 0), v);
-        cp_async16(vs + d, a.pv.v + (v ? o : 0), v);
+          for (int i = 0; i < 16 / RPI; ++i) {
+            cp_async16_all(ks + dst(i), k);
+            cp_async16_all(vs + dst(i), v);
+            k += step;
+            v += step;
+          }
+        } else {
+#pragma unroll 1
+          for (int i = 0; i < 16 / RPI; ++i) {
+            const bool there = i * RPI + r0 < n;
+            cp_async16(ks + dst(i), there ? k : a.pv.k, there);
+            cp_async16(vs + dst(i), there ? v : a.pv.v, there);
+            k += step;
+            v += step;
+          }
+        }
+      } else {
+        const int page = __shfl_sync(0xffffffffu, id, (p.chunk - base) * 16 + (lane & 15)), row = __shfl_sync(0xffffffffu, rem, (p.chunk - base) * 16 + (lane & 15));
+        live = __ballot_sync(0xffffffffu, page >= 0) & 0xffffu;
+        const long long off = page < 0 ? 0 : (long long)page * a.pv.page_stride + (long long)row * a.pv.row_stride + (long long)p.kvh * a.pv.head_stride;
+#pragma unroll
+        for (int i = 0; i < 16 / RPI; ++i) {
+          const int r = i * RPI + r0;
+          const long long o = __shfl_sync(0xffffffffu, off, r) * (int)sizeof(T) + ch * 16;
+          const bool there = (live >> r) & 1;
+          cp_async16(ks + dst(i), a.pv.k + (there ? o : 0), there);
+          cp_async16(vs + dst(i), a.pv.v + (there ? o : 0), there);
+        }
       }
       first = --p.left == 0;
       if (first) {
         p = pa_place(a, pre, p.next(), hi);
         if (p.left > 0) begin();
-      } else if (++p.chunk == base + 2) {
-        base += 2;
-        ids = ids2;
-        ids2 = ask(base + 2);
+      } else if (++p.chunk == base + WINDOW) {
+        base += WINDOW;
+        id = id2;
+        rem = rem2;
+        ask(base + WINDOW, id2, rem2);
       }
     }
     cp_async_commit();
@@ -251,10 +295,10 @@ struct PaLoader {
 };
 
 // The ring of a warp: which stage is next, what is in flight.
-template <typename T, int DH>
+template <typename T, int DH, bool A16>
 struct PaRing {
   using S = PaSmem<T, DH>;
-  PaLoader<T, DH> ld;
+  PaLoader<T, DH, A16> ld;
   char *q_tiles, *ring;
   int q_tile_bytes, stage = 0, tile = 0;
   unsigned live[S::STAGES];     // masks of the stages in flight, oldest first
@@ -287,8 +331,13 @@ struct PaRing {
   }
 };
 
-// e^(x) of the online softmax in log2 units; -inf - -inf (nothing seen yet) counts as nothing.
-__device__ __forceinline__ float pa_scale(float m_old, float m_new) { return m_old == -INFINITY ? 0.f : exp2f(m_old - m_new); }
+__device__ __forceinline__ float pa_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// 2^(m_old - m_new) of the online softmax; -inf - -inf (nothing seen yet) counts as nothing.
+__device__ __forceinline__ float pa_scale(float m_old, float m_new) { return m_old == -INFINITY ? 0.f : pa_exp2(m_old - m_new); }
 
 // A lane's share of a result row: VEC = DH / 32 neighbouring elements, sums o over weights that sum to l.
 template <typename T, int DH>
@@ -456,8 +505,11 @@ __device__ __forceinline__ void pa_empty(const PagedAttnArgs& a, const int* pre)
 // ---- bf16: tensor cores --------------------------------------------------------------------------------------------------
 // Softmax weights are fed to the P V product as the sum of two bf16 numbers (16 bits of mantissa): the tensor pipe has the time,
 // and the output is then as exact as one with fp32 weights.
-template <int DH>
-__global__ void __launch_bounds__(PA_THREADS, 2) k_paged_attn_mma(const PagedAttnArgs a) {
+// The maximum is raised only where a score is more than 2^PA_LAZY times the weight of the present one (the sums have room for that), so that most
+// chunks need neither its exchange over the lanes nor a rescale.
+constexpr float PA_LAZY = 8.f;
+template <int DH, bool A16>
+__global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 2)) k_paged_attn_mma(const PagedAttnArgs a) {
   extern __shared__ __align__(128) char pa_smem[];
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   int* pre = reinterpret_cast<int*>(pa_smem + PaSmem<bf16, DH>::pre(a.q_rows, a.merge_rows));
@@ -472,21 +524,31 @@ __global__ void __launch_bounds__(PA_THREADS, 2) k_paged_attn_mma(const PagedAtt
   __shared__ PaPlace cut[2];
   if (threadIdx.x < 2) cut[threadIdx.x].left = 0;
 
-  PaRing<bf16, DH> ring(a, pre, hi, p, pa_smem);
+  PaRing<bf16, DH, A16> ring(a, pre, hi, p, pa_smem);
+  // this lane's rows and chunks of the K and V tiles (ldmatrix); chunk c lies at c ^ (row & 7): further chunks are the same address with
+  // bits 5, 6 flipped, or 128 bytes on
+  const uint32_t k_at = pa_at<bf16, DH>(lane & 7, lane >> 3), v_at = pa_at<bf16, DH>((lane & 7) + ((lane >> 3) & 1) * 8, lane >> 4);
+  const float lazy = PA_LAZY / a.scale_log2;
   for (; p.left > 0; p = pa_place(a, pre, p.next(), hi)) {
     // ---- a unit, or the part of it that belongs to this run
     const RowSpan rs = pg_rows(a.pv, a.row_off, p.b, a.max_rows, a.n_rows);
     const int n_real = min(PA_ROWS, rs.n * a.group - p.rt * PA_ROWS);
-    int row[2], head[2];
-    bool real[2];
+    float* score[2] = {nullptr, nullptr};         // where the two rows' scores go
+    if (a.scores) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) real[h] = pa_row(a, rs, p, g + 8 * h, row[h], head[h]);
+      for (int h = 0; h < 2; ++h) {
+        int row, head;
+        if (pa_row(a, rs, p, g + 8 * h, row, head)) score[h] = a.scores + ((long long)row * a.hq + head) * pg_capacity(a.pv) + 2 * t;
+      }
+    }
     uint32_t qf[DH / 16][4];
     float o[DH / 8][4];
 #pragma unroll
     for (int i = 0; i < DH / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    // per row: the maximum (unscaled), where it is raised, what is added to a scaled score, the sum of this lane's weights
+    float m[2] = {-INFINITY, -INFINITY}, limit[2] = {-INFINITY, -INFINITY}, shift[2] = {0.f, 0.f}, l[2] = {0.f, 0.f};
 
+#pragma unroll 1
     for (int k = 0; k < p.left; ++k) {
       char* rows;
       const unsigned mask = ring.turn(rows);
@@ -510,68 +572,67 @@ __global__ void __launch_bounds__(PA_THREADS, 2) k_paged_attn_mma(const PagedAtt
 #pragma unroll
         for (int kk = 0; kk < DH / 16; kk += 2) {
           uint32_t b0, b1, b2, b3;
-          ldsm_x4(ks + pa_at<bf16, DH>(j * 8 + (lane & 7), kk * 2 + (lane >> 3)), b0, b1, b2, b3);
+          ldsm_x4(ks + (k_at ^ ((kk * 2 & 4) << 4)) + j * 8 * DH * 2 + (kk >= 4 ? 128 : 0), b0, b1, b2, b3);
           mma_bf16(s[j], qf[kk][0], qf[kk][1], qf[kk][2], qf[kk][3], b0, b1);
           mma_bf16(s2, qf[kk + 1][0], qf[kk + 1][1], qf[kk + 1][2], qf[kk + 1][3], b2, b3);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[j][e] += s2[e];
       }
-      float mx[2] = {-INFINITY, -INFINITY};
+      if (mask != 0xffffu) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s[j][e] = (mask >> (j * 8 + 2 * t + (e & 1))) & 1 ? s[j][e] * a.scale_log2 : -INFINITY;
-          mx[e >> 1] = fmaxf(mx[e >> 1], s[j][e]);
-        }
+          for (int e = 0; e < 4; ++e)
+            if (!((mask >> (j * 8 + 2 * t + (e & 1))) & 1)) s[j][e] = -INFINITY;
+      }
       if (a.scores) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-          if (real[h]) {
-            float* dst = a.scores + ((long long)row[h] * a.hq + head[h]) * pg_capacity(a.pv) + j0 + 2 * t;
+          if (score[h]) {
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
               for (int e = 0; e < 2; ++e)
-                if (j0 + j * 8 + 2 * t + e < p.len) dst[j * 8 + e] = s[j][2 * h + e];
+                if (j0 + j * 8 + 2 * t + e < p.len) score[h][j0 + j * 8 + e] = s[j][2 * h + e] * a.scale_log2;
           }
       }
-      float corr[2];
+      float mx[2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 1));
-        mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 2));
-        const float m_new = fmaxf(m[h], mx[h]);
-        corr[h] = pa_scale(m[h], m_new);
-        m[h] = m_new;
+      for (int h = 0; h < 2; ++h) mx[h] = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
+      if (__any_sync(0xffffffffu, mx[0] > limit[0] || mx[1] > limit[1])) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 1));
+          mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 2));
+          const float top = fmaxf(m[h], mx[h]), corr = m[h] == -INFINITY ? 0.f : pa_exp2((m[h] - top) * a.scale_log2);
+          m[h] = top;
+          limit[h] = top + lazy;
+          shift[h] = top == -INFINITY ? 0.f : -top * a.scale_log2;
+          l[h] *= corr;
+#pragma unroll
+          for (int i = 0; i < DH / 8; ++i) {
+            o[i][2 * h] *= corr;
+            o[i][2 * h + 1] *= corr;
+          }
+        }
       }
       uint32_t hi_[4], lo_[4];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        l[h] *= corr[h];
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const float x = s[j][2 * h], y = s[j][2 * h + 1];
-          const float p0 = x == -INFINITY ? 0.f : exp2f(x - m[h]), p1 = y == -INFINITY ? 0.f : exp2f(y - m[h]);
+          const float p0 = pa_exp2(fmaf(s[j][2 * h], a.scale_log2, shift[h])), p1 = pa_exp2(fmaf(s[j][2 * h + 1], a.scale_log2, shift[h]));
           l[h] += p0 + p1;
-          const __nv_bfloat162 ph = __floats2bfloat162_rn(p0, p1);
-          hi_[j * 2 + h] = *reinterpret_cast<const uint32_t*>(&ph);
-          lo_[j * 2 + h] = pack_bf16(p0 - __bfloat162float(ph.x), p1 - __bfloat162float(ph.y));
+          const uint32_t x = pack_bf16(p0, p1);
+          hi_[j * 2 + h] = x;
+          lo_[j * 2 + h] = pack_bf16(p0 - __uint_as_float(x << 16), p1 - __uint_as_float(x & 0xffff0000u));
         }
-      }
-      if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
-#pragma unroll
-        for (int i = 0; i < DH / 8; ++i) {
-          o[i][0] *= corr[0]; o[i][1] *= corr[0];
-          o[i][2] *= corr[1]; o[i][3] *= corr[1];
-        }
-      }
       // O += P V
 #pragma unroll
       for (int nt = 0; nt < DH / 8; nt += 2) {
         uint32_t b0, b1, b2, b3;
-        ldsm_x4_t(vs + pa_at<bf16, DH>((lane & 7) + ((lane >> 3) & 1) * 8, nt + (lane >> 4)), b0, b1, b2, b3);
+        ldsm_x4_t(vs + (v_at ^ ((nt & 6) << 4)) + (nt >= 8 ? 128 : 0), b0, b1, b2, b3);
         mma_bf16(o[nt], hi_[0], hi_[1], hi_[2], hi_[3], b0, b1);
         mma_bf16(o[nt + 1], hi_[0], hi_[1], hi_[2], hi_[3], b2, b3);
         mma_bf16(o[nt], lo_[0], lo_[1], lo_[2], lo_[3], b0, b1);
@@ -582,6 +643,7 @@ __global__ void __launch_bounds__(PA_THREADS, 2) k_paged_attn_mma(const PagedAtt
     for (int h = 0; h < 2; ++h) {
       l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
       l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+      m[h] *= a.scale_log2;
     }
     pa_finish<bf16, DH>(a, p, rs, lo, cut, pa_smem, [&](int i0, int n, float* dst, float2* ml) {
 #pragma unroll
@@ -600,8 +662,8 @@ __global__ void __launch_bounds__(PA_THREADS, 2) k_paged_attn_mma(const PagedAtt
 // ---- fp32: CUDA cores ----------------------------------------------------------------------------------------------------
 // Scores: a lane takes one slot and half of the dimensions; P V: a lane takes DH / 32 dimensions.  A kernel for every power of two of
 // rows: the work a slot costs goes with the rows, and a branch a row and slot (16 of them with one real row) took ten times the bytes' time.
-template <int DH, int NR>
-__global__ void __launch_bounds__(PA_THREADS) k_paged_attn_simt(const PagedAttnArgs a) {
+template <int DH, int NR, bool A16>
+__global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 4)) k_paged_attn_simt(const PagedAttnArgs a) {
   extern __shared__ __align__(128) char pa_smem[];
   constexpr int VEC = DH / 32;                  // dimensions of a lane in P V
   constexpr int PARTS = NR <= 2 ? 4 : 1;        // independent sums of a score (few rows: the chain of FMAs would be the time)
@@ -618,7 +680,7 @@ __global__ void __launch_bounds__(PA_THREADS) k_paged_attn_simt(const PagedAttnA
   __shared__ PaPlace cut[2];
   if (threadIdx.x < 2) cut[threadIdx.x].left = 0;
 
-  PaRing<float, DH> ring(a, pre, hi, p, pa_smem);
+  PaRing<float, DH, A16> ring(a, pre, hi, p, pa_smem);
   const int key = lane & 15, half = lane >> 4;
   for (; p.left > 0; p = pa_place(a, pre, p.next(), hi)) {
     const RowSpan rs = pg_rows(a.pv, a.row_off, p.b, a.max_rows, a.n_rows);
@@ -672,7 +734,7 @@ __global__ void __launch_bounds__(PA_THREADS) k_paged_attn_simt(const PagedAttnA
         const float m_new = fmaxf(m[r], warp_max(x));
         const float corr = pa_scale(m[r], m_new);
         m[r] = m_new;
-        pr[r] = x == -INFINITY ? 0.f : exp2f(x - m_new);
+        pr[r] = x == -INFINITY ? 0.f : pa_exp2(x - m_new);
         l[r] = l[r] * corr + pr[r];
 #pragma unroll
         for (int e = 0; e < VEC; ++e) o[r][e] *= corr;
