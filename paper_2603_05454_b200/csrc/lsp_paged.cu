@@ -128,8 +128,12 @@ cudaError_t launch_attention(const PagedAttnArgs& a0, int tiles, cudaStream_t st
   a.n_cta = (int)std::min<long long>(most, std::min(n_per_sm * n_sm, pa_max_ctas(DH)));
   e = launch_k(1, kern, dim3(a.n_cta), dim3(PA_THREADS), (size_t)smem, stream, a);
   if (e != cudaSuccess || !a.scores) return e;
-  const int key_blocks = (int)((cap + PW_KEYS - 1) / PW_KEYS);
-  return launch_k(1, k_paged_weights, dim3(a.pv.batch * a.pv.hkv * key_blocks), dim3(PW_THREADS), (size_t)a.max_rows * a.group * 4, stream, a, key_blocks);
+  // a slot a thread, and four where that still leaves four blocks an SM
+  const long long units = (long long)a.pv.batch * a.pv.hkv;
+  const int kpt = units * ((cap + 4 * PW_THREADS - 1) / (4 * PW_THREADS)) >= 4 * n_sm ? 4 : 1;
+  const int key_blocks = (int)((cap + kpt * PW_THREADS - 1) / (kpt * PW_THREADS));
+  return launch_k(1, kpt == 4 ? k_paged_weights<4> : k_paged_weights<1>, dim3((unsigned)(units * key_blocks)), dim3(PW_THREADS), (size_t)a.max_rows * a.group * 4,
+                  stream, a, key_blocks);
 }
 
 // The selection's launch: 1024 threads a CTA, a cluster of CTAs per unit while that fills no more than the SMs and leaves each CTA 2048 slots
@@ -218,7 +222,7 @@ int lsp_paged_attention(const lsp_paged_kv* kv, const void* q, long long ldq, in
   a.group = n_heads / kv->n_kv_heads;
   const long long rows_unit = (long long)max_rows * a.group, tiles = (rows_unit + PA_ROWS - 1) / PA_ROWS;
   const long long cap = (long long)kv->max_pages * kv->page_size, units = tiles * kv->batch * kv->n_kv_heads;
-  if ((long long)kv->batch * kv->n_kv_heads * (cap / PW_KEYS + 1) > 0x7fffffffll || units * (cap / PA_CHUNK + 1 + PA_UNIT_COST) > 0x7fffffffll)
+  if ((long long)kv->batch * kv->n_kv_heads * (cap / PW_THREADS + 1) > 0x7fffffffll || units * (cap / PA_CHUNK + 1 + PA_UNIT_COST) > 0x7fffffffll)
     return e.fail(LSP_ERR_SHAPE, "%s: batch x heads x rows x slots too large for one call", who);
   if (weights_out && rows_unit > 8192) return e.fail(LSP_ERR_SHAPE, "%s: weights of more than 8192 (row, head) pairs per KV head", who);
   if (n_rows == 0 && !weights_out) return LSP_OK;

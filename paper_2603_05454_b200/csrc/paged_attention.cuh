@@ -29,9 +29,9 @@ constexpr int PA_MAX_BATCH = 1024;
 // CTAs of a launch at most (workspaces are sized by it), and on an SM: those that 64 warps' registers allow, so that 128 KB are in flight
 __host__ __device__ constexpr int pa_max_ctas(int dh) { return dh == 64 ? 1024 : 512; }
 __host__ __device__ constexpr int pa_ctas_sm(int dh, int esz) { return dh == 64 && esz == 2 ? 4 : dh == 128 && esz == 4 ? 1 : 2; }
-constexpr int PA_UNIT_COST = 2;         // what a unit costs besides its chunks, in chunks (queries, adding the warps' parts)
+constexpr int PA_UNIT_COST = 3;         // what a unit costs besides its chunks, in chunks (queries, adding the warps' parts)
 constexpr int PW_THREADS = 256;
-constexpr int PW_KEYS = 1024;           // slots of a weights block
+constexpr int PW_AHEAD = 8;             // scores of a thread under way at once
 
 struct PagedAttnArgs {
   PagedView pv;
@@ -105,6 +105,18 @@ __device__ __forceinline__ void pa_prefix(const PagedAttnArgs& a, int* pre) {
   }
   if (B > 32) __syncthreads();
   else __syncwarp();
+}
+
+// Ahead of the wait for the preceding kernel: lengths, offsets and page table into L2 (a line a thread, dealt over the grid).  They are
+// read only behind it, and the chain lengths -> pages -> rows is what a launch begins with.
+__device__ __forceinline__ void pa_prefetch(const PagedAttnArgs& a) {
+  const int n_len = (a.pv.batch * 4 + 127) / 128, n_off = a.row_off ? n_len : 0;
+  const int n_table = a.pv.table ? (int)(((long long)a.pv.batch * a.pv.max_pages * 4 + 127) / 128) : 0;
+  for (int i = threadIdx.x * gridDim.x + blockIdx.x; i < n_len + n_off + n_table; i += gridDim.x * blockDim.x) {
+    const char* at = i < n_len ? (const char*)a.lens + i * 128 : i < n_len + n_off ? (const char*)a.row_off + (i - n_len) * 128
+                                                                                : (const char*)a.pv.table + (long long)(i - n_len - n_off) * 128;
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
+  }
 }
 
 // How the numbers are dealt: CTA i of n (those that get at least one) has numbers [run(i), run(i + 1)), run(i) = floor(total i / n).
@@ -413,7 +425,7 @@ __device__ __forceinline__ void pa_finish(const PagedAttnArgs& a, const PaPlace&
 
 // The end of the run: its parts of cut units are there; the last CTA of a unit to say so adds them all, in their order.  A warp takes a
 // row at a time, 32 parts' (m, l) on its lanes and PA_AHEAD parts' o under way; the code is short because it is fetched cold.
-constexpr int PA_AHEAD = 16;
+constexpr int PA_AHEAD = 8;
 template <typename T, int DH>
 __device__ __forceinline__ void pa_join(const PagedAttnArgs& a, const PaDeal& deal, const PaPlace* cut) {
   constexpr int VEC = DH / 32;
@@ -455,15 +467,9 @@ __device__ __forceinline__ void pa_join(const PagedAttnArgs& a, const PaDeal& de
         const int k = min(k0 + lane, n - 1);
         const int slot = (2 * (i0 + k) + (k == 0 ? parts[which][1] : 0)) * PA_ROWS + r;
         const float2 x = __ldcg(a.part_ml + slot);
-        const float top = fmaxf(m, warp_max(x.x)), f0 = pa_scale(m, top);
-        const float f = k0 + lane < n ? pa_scale(x.x, top) : 0.f;
-        m = top;
-        l = l * f0 + warp_sum(x.y * f);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) o[e] *= f0;
+        float y[PA_AHEAD][VEC], f = 0.f;
 #pragma unroll 1
         for (int q = 0; q < 32 && k0 + q < n; q += PA_AHEAD) {
-          float y[PA_AHEAD][VEC];
 #pragma unroll
           for (int i = 0; i < PA_AHEAD; ++i) {
             const float* src = a.part_o + (long long)__shfl_sync(0xffffffffu, slot, q + i) * DH + lane * VEC;
@@ -474,6 +480,14 @@ __device__ __forceinline__ void pa_join(const PagedAttnArgs& a, const PaDeal& de
               const float2 z = __ldcg(reinterpret_cast<const float2*>(src));
               y[i][0] = z.x; y[i][1] = z.y;
             }
+          }
+          if (q == 0) {                                // (while they are under way)
+            const float top = fmaxf(m, warp_max(x.x)), f0 = pa_scale(m, top);
+            f = k0 + lane < n ? pa_scale(x.x, top) : 0.f;
+            m = top;
+            l = l * f0 + warp_sum(x.y * f);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) o[e] *= f0;
           }
 #pragma unroll
           for (int i = 0; i < PA_AHEAD; ++i) {
@@ -513,7 +527,9 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 2)) k_paged_attn_mm
   extern __shared__ __align__(128) char pa_smem[];
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   int* pre = reinterpret_cast<int*>(pa_smem + PaSmem<bf16, DH>::pre(a.q_rows, a.merge_rows));
-  pdl_begin();
+  pdl_release();
+  pa_prefetch(a);
+  pdl_wait();
   pa_prefix(a, pre);
   pa_empty<bf16, DH>(a, pre);
   const PaDeal deal(pre[a.pv.batch], a.n_cta);
@@ -669,7 +685,9 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 4)) k_paged_attn_si
   constexpr int PARTS = NR <= 2 ? 4 : 1;        // independent sums of a score (few rows: the chain of FMAs would be the time)
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   int* pre = reinterpret_cast<int*>(pa_smem + PaSmem<float, DH>::pre(a.q_rows, a.merge_rows));
-  pdl_begin();
+  pdl_release();
+  pa_prefetch(a);
+  pdl_wait();
   pa_prefix(a, pre);
   pa_empty<float, DH>(a, pre);
   const PaDeal deal(pre[a.pv.batch], a.n_cta);
@@ -774,30 +792,55 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 4)) k_paged_attn_si
 }
 
 // ---- gathered weights ----------------------------------------------------------------------------------------------------
-// PW_KEYS slots of one (sequence, KV head) a block, from the scores that the kernel above left: e^{s - lse} of all rows and heads of the group.
+// KPT slots a thread of one (sequence, KV head), from the scores that the kernel above left: e^{s - lse} of all rows and heads of the group.
+// Bound by latency where there are few slots, by the scores' bytes (4 a slot and row) where there are many: PW_AHEAD scores are under way at
+// once.
+template <int KPT>
 __global__ void __launch_bounds__(PW_THREADS) k_paged_weights(const PagedAttnArgs a, int key_blocks) {
+  constexpr int ROWS = PW_AHEAD / KPT;
   extern __shared__ float lse2[];                 // [max_rows * group]
   pdl_begin();
   int u = blockIdx.x;
-  const int j0 = (u % key_blocks) * PW_KEYS;
+  const int j0 = (u % key_blocks) * (KPT * PW_THREADS);
   u /= key_blocks;
   const int kvh = u % a.pv.hkv, b = u / a.pv.hkv;
   const int len = pg_len(a.pv, a.lens[b]), cap = pg_capacity(a.pv);
-  if (j0 >= len) return;
   const RowSpan rs = pg_rows(a.pv, a.row_off, b, a.max_rows, a.n_rows);
+  if (j0 >= len) return;
   const int n = rs.n * a.group;
   for (int x = threadIdx.x; x < n; x += PW_THREADS) {
     const float l = a.row_lse[(long long)(rs.first + x / a.group) * a.hq + kvh * a.group + x % a.group];
     lse2[x] = l == -INFINITY ? INFINITY : l;      // a row that saw nothing has no weight
   }
-  __syncthreads();
   const long long base = ((long long)b * a.pv.hkv + kvh) * cap;
-  for (int j = j0 + threadIdx.x; j < min(j0 + PW_KEYS, len); j += PW_THREADS) {
-    float s = a.weights_in ? a.weights_in[base + j] : 0.f;
-    for (int x = 0; x < n; ++x)
-      s += exp2f(a.scores[((long long)(rs.first + x / a.group) * a.hq + kvh * a.group + x % a.group) * cap + j] - lse2[x]);
-    a.weights_out[base + j] = s;
+  const int j = j0 + threadIdx.x;
+  float sum[KPT];
+#pragma unroll
+  for (int k = 0; k < KPT; ++k) sum[k] = j + k * PW_THREADS < len && a.weights_in ? a.weights_in[base + j + k * PW_THREADS] : 0.f;
+  __syncthreads();
+  // scores of row x of the group's: `heads` of a row lie one behind the other, the next row's a.hq heads on
+  const float* src = a.scores + ((long long)rs.first * a.hq + kvh * a.group) * cap + j;
+  const long long wrap = (long long)(a.hq - a.group + 1) * cap;
+  int h = 0;
+  float add[KPT] = {};
+  for (int x = 0; x < n; x += ROWS) {
+    float s[ROWS][KPT];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+#pragma unroll
+      for (int k = 0; k < KPT; ++k) s[i][k] = x + i < n && j + k * PW_THREADS < len ? __ldcg(src + k * PW_THREADS) : -INFINITY;
+      const bool last = ++h == a.group;
+      src += last ? wrap : cap;
+      h = last ? 0 : h;
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+      for (int k = 0; k < KPT; ++k) add[k] += pa_exp2(s[i][k] - lse2[min(x + i, n - 1)]);
   }
+#pragma unroll
+  for (int k = 0; k < KPT; ++k)
+    if (j + k * PW_THREADS < len) a.weights_out[base + j + k * PW_THREADS] = sum[k] + add[k];
 }
 
 }  // namespace lsp
