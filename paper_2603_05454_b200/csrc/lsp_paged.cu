@@ -187,7 +187,14 @@ int lsp_paged_append(const lsp_paged_kv* kv, const void* k_new, const void* v_ne
   a.seen_out = seen_out;
   a.weights = weights;
   a.pos = pos;
-  const cudaError_t ce = launch_k(1, k_paged_append, dim3(n_rows + 1), dim3(PP_THREADS), 0, (cudaStream_t)cuda_stream, a);
+  // rows of a block: what its threads hold, as long as that leaves four blocks an SM
+  const int row_bytes = 2 * kv->n_kv_heads * a.head_bytes;
+  int dev = 0, n_sm = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return e.fail(LSP_ERR_CUDA, "%s: no usable current device", who);
+  a.rows_block = std::max(1, std::min({PP_ROWS, PP_THREADS * PP_VEC * 16 / row_bytes, n_rows / (4 * n_sm)}));
+  const cudaError_t ce = launch_k(1, k_paged_append, dim3((n_rows + a.rows_block - 1) / a.rows_block + 1), dim3(PP_THREADS), row_off ? (size_t)kv->batch * 4 : 0,
+                                  (cudaStream_t)cuda_stream, a);
   if (ce != cudaSuccess) return e.fail(LSP_ERR_CUDA, "%s: launch failed (%s)", who, cudaGetErrorString(ce));
   return LSP_OK;
 }

@@ -7,9 +7,11 @@ namespace lsp {
 
 // ---- append --------------------------------------------------------------------------------------------------------------
 // Row i of sequence b (packed row row_off[b] + i) goes to slot lens[b] + i.  Bound by HBM for prompts and by latency for single
-// tokens: a thread has its share of the row in registers before it knows where the row goes.
+// tokens: a block has its rows under way to registers (16 KB, a row or as many as that is) while it finds their places (offsets -> lengths ->
+// pages).  (Longer-lived blocks, a warp a half row at a time, were slower: 3063 rows of 16 KB 24.6 us, 19.8 so.)
 constexpr int PP_THREADS = 256;
 constexpr int PP_VEC = 4;               // 16-byte pieces of a thread that are under way at once
+constexpr int PP_ROWS = 32;             // rows of a block at most
 
 struct PagedAppendArgs {
   PagedView pv;
@@ -17,18 +19,21 @@ struct PagedAppendArgs {
   long long ld_new;                     // bytes
   const int *lens, *row_off, *seen;
   int max_rows, n_rows, esz, head_bytes;      // head_bytes = head_dim * esz
+  int rows_block;                       // rows of a block
   int* lens_out;
   int* seen_out;
   float* weights;
   int* pos;
 };
 
-// Blocks [0, n_rows): a packed row each.  The last block: the lengths.
+// Blocks ahead of the last: rows_block packed rows each.  The last block: the lengths.
 __global__ void __launch_bounds__(PP_THREADS) k_paged_append(const PagedAppendArgs a) {
-  __shared__ int place[4];              // sequence, slot, page, position
+  extern __shared__ int offsets[];      // [batch] row_off
+  __shared__ int seqs[PP_ROWS], slots[PP_ROWS], poss[PP_ROWS];
+  __shared__ long long places[PP_ROWS]; // bytes, -1: nowhere
   pdl_begin();
   const int B = a.pv.batch, cap = pg_capacity(a.pv);
-  if ((int)blockIdx.x == a.n_rows) {
+  if (blockIdx.x == gridDim.x - 1) {
     for (int b = threadIdx.x; b < B; b += PP_THREADS) {
       const RowSpan rs = pg_rows(a.pv, a.row_off, b, a.max_rows, a.n_rows);
       const int n = pg_len(a.pv, a.lens[b]);
@@ -42,72 +47,86 @@ __global__ void __launch_bounds__(PP_THREADS) k_paged_append(const PagedAppendAr
     }
     return;
   }
-  const int r = blockIdx.x;
-  const int row_bytes = a.pv.hkv * a.head_bytes, pieces = row_bytes / 16;
-  const char* ksrc = a.k_new + (long long)r * a.ld_new;
-  const char* vsrc = a.v_new + (long long)r * a.ld_new;
+  const int r0 = blockIdx.x * a.rows_block, n = min(a.rows_block, a.n_rows - r0);
+  const int pieces = a.pv.hkv * a.head_bytes / 16, total = n * 2 * pieces;      // of a row's K or V; of the block
+  // piece c of the block: row, K or V, piece of that
+  struct Piece { int row, v, c; };
+  auto piece = [&](int c) {
+    Piece p;
+    p.row = a.rows_block == 1 ? 0 : c / (2 * pieces);
+    p.c = c - p.row * 2 * pieces;
+    p.v = p.c >= pieces ? 1 : 0;
+    p.c -= p.v ? pieces : 0;
+    return p;
+  };
+  auto load = [&](int c) {
+    const Piece p = piece(c);
+    return reinterpret_cast<const uint4*>((p.v ? a.v_new : a.k_new) + (long long)(r0 + p.row) * a.ld_new)[p.c];
+  };
   uint4 x[PP_VEC];
 #pragma unroll
   for (int i = 0; i < PP_VEC; ++i) {
-    const int c = threadIdx.x + i * PP_THREADS;
-    if (c < 2 * pieces) x[i] = c < pieces ? reinterpret_cast<const uint4*>(ksrc)[c] : reinterpret_cast<const uint4*>(vsrc)[c - pieces];
+    const int c = i * PP_THREADS + threadIdx.x;
+    if (c < total) x[i] = load(c);
   }
-  // the sequence: the last one that starts at or ahead of row r (of those that start there, the one with rows)
-  int b = 0;
-  if (!a.row_off) {
-    b = r / a.max_rows;
-  } else {
-    int n = 0;
-    for (int b0 = 0; b0 < B; b0 += PP_THREADS) {
-      const int i = b0 + threadIdx.x;
-      n += __syncthreads_count(i < B && a.row_off[i] <= r);
+  if (a.row_off) {
+    for (int b = threadIdx.x; b < B; b += PP_THREADS) offsets[b] = a.row_off[b];
+    __syncthreads();
+  }
+  if (threadIdx.x < n) {
+    const int r = r0 + threadIdx.x;
+    long long place = -1;
+    int b, slot = 0, position = 0;
+    if (!a.row_off) {
+      b = r / a.max_rows;
+    } else {                            // the last sequence that starts at or ahead of the row (of those that start there, the one with rows)
+      int lo = -1, up = B;
+      while (up - lo > 1) {
+        const int mid = (lo + up) >> 1;
+        if (offsets[mid] <= r) lo = mid; else up = mid;
+      }
+      b = lo;
     }
-    b = n - 1;
-  }
-  if (threadIdx.x == 0) {
-    place[0] = -1;
     if (b >= 0) {
       const RowSpan rs = pg_rows(a.pv, a.row_off, b, a.max_rows, a.n_rows);
-      const int n = pg_len(a.pv, a.lens[b]), i = r - rs.first;
-      if (i >= 0 && i < rs.n && n + i < cap) {
-        const int id = pg_page(a.pv, b, n + i);
-        if (id >= 0) {
-          place[0] = b;
-          place[1] = n + i;
-          place[2] = id;
-          place[3] = a.pos ? (a.seen ? a.seen[b] : n) + i : 0;
-        }
+      const int len = pg_len(a.pv, a.lens[b]), i = r - rs.first;
+      if (i >= 0 && i < rs.n && len + i < cap) {
+        slot = len + i;
+        const int id = pg_page(a.pv, b, slot);
+        if (id >= 0) place = ((long long)id * a.pv.page_stride + (long long)(slot % a.pv.page) * a.pv.row_stride) * a.esz;
+        position = a.seen ? a.seen[b] + i : slot;
       }
     }
+    places[threadIdx.x] = place;
+    seqs[threadIdx.x] = b;
+    slots[threadIdx.x] = slot;
+    poss[threadIdx.x] = position;
   }
   __syncthreads();
-  if (place[0] < 0) return;
-  b = place[0];
-  const int slot = place[1];
-  const long long at = (long long)place[2] * a.pv.page_stride + (long long)(slot % a.pv.page) * a.pv.row_stride;
-  const int per_head = a.head_bytes / 16;
-  for (int c0 = 0; c0 < 2 * pieces; c0 += PP_VEC * PP_THREADS) {
-    if (c0 > 0) {
+  const int shift = 31 - __clz(a.head_bytes / 16);    // pieces of a head: 8, 16 or 32
+  for (int c0 = threadIdx.x; c0 < total; c0 += PP_VEC * PP_THREADS) {
+    if (c0 >= PP_VEC * PP_THREADS) {
 #pragma unroll
-      for (int i = 0; i < PP_VEC; ++i) {
-        const int c = c0 + threadIdx.x + i * PP_THREADS;
-        if (c < 2 * pieces) x[i] = c < pieces ? reinterpret_cast<const uint4*>(ksrc)[c] : reinterpret_cast<const uint4*>(vsrc)[c - pieces];
-      }
+      for (int i = 0; i < PP_VEC; ++i)
+        if (c0 + i * PP_THREADS < total) x[i] = load(c0 + i * PP_THREADS);
     }
 #pragma unroll
     for (int i = 0; i < PP_VEC; ++i) {
-      const int c = c0 + threadIdx.x + i * PP_THREADS;
-      if (c >= 2 * pieces) break;
-      const int d = c < pieces ? c : c - pieces;
-      char* pool = c < pieces ? a.pv.k : a.pv.v;
-      *reinterpret_cast<uint4*>(pool + (at + (long long)(d / per_head) * a.pv.head_stride) * a.esz + (d % per_head) * 16) = x[i];
+      if (c0 + i * PP_THREADS >= total) break;
+      const Piece p = piece(c0 + i * PP_THREADS);
+      const long long place = places[p.row];
+      if (place < 0) continue;
+      char* dst = (p.v ? a.pv.v : a.pv.k) + place + (long long)(p.c >> shift) * a.pv.head_stride * a.esz + (p.c & ((1 << shift) - 1)) * 16;
+      *reinterpret_cast<uint4*>(dst) = x[i];
     }
   }
   if (a.weights || a.pos)
-    for (int h = threadIdx.x; h < a.pv.hkv; h += PP_THREADS) {
-      const long long w = ((long long)b * a.pv.hkv + h) * cap + slot;
-      if (a.weights) a.weights[w] = 0.f;
-      if (a.pos) a.pos[w] = place[3];
+    for (int i = threadIdx.x; i < n * a.pv.hkv; i += PP_THREADS) {
+      const int r = i % n, h = i / n;                // (rows of a sequence lie one behind the other in a head's array)
+      if (places[r] < 0) continue;
+      const long long at = ((long long)seqs[r] * a.pv.hkv + h) * cap + slots[r];
+      if (a.weights) a.weights[at] = 0.f;
+      if (a.pos) a.pos[at] = poss[r];
     }
 }
 
