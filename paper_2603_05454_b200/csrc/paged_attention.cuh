@@ -425,7 +425,7 @@ __device__ __forceinline__ void pa_finish(const PagedAttnArgs& a, const PaPlace&
 
 // The end of the run: its parts of cut units are there; the last CTA of a unit to say so adds them all, in their order.  A warp takes a
 // row at a time, 32 parts' (m, l) on its lanes and PA_AHEAD parts' o under way; the code is short because it is fetched cold.
-constexpr int PA_AHEAD = 8;
+constexpr int PA_AHEAD = 16;
 template <typename T, int DH>
 __device__ __forceinline__ void pa_join(const PagedAttnArgs& a, const PaDeal& deal, const PaPlace* cut) {
   constexpr int VEC = DH / 32;
