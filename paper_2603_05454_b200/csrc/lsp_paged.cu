@@ -54,6 +54,12 @@ int check_view(const Err& e, const char* who, const lsp_paged_kv* kv, PagedView*
   return LSP_OK;
 }
 
+// A launch or attribute call that failed: the message, and no error left behind for the caller's next CUDA call.
+int cuda_failed(const Err& e, const char* who, cudaError_t ce) {
+  cudaGetLastError();
+  return e.fail(LSP_ERR_CUDA, "%s: launch failed (%s)", who, cudaGetErrorString(ce));
+}
+
 int check_rows(const Err& e, const char* who, const lsp_paged_kv* kv, const int32_t* row_off, int max_rows, int n_rows) {
   if (max_rows < 1 || n_rows < 0) return e.fail(LSP_ERR_ARG, "%s: max_rows %d or n_rows %d", who, max_rows, n_rows);
   if (!row_off && (long long)kv->batch * max_rows != n_rows)
@@ -120,8 +126,8 @@ cudaError_t launch_attention(const PagedAttnArgs& a0, int tiles, cudaStream_t st
   int dev = 0, n_sm = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev);
-  // (the limit belongs to the CUDA context: set with every call)
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  // (the limit belongs to the CUDA context: set with every call, to the same value, since another thread may be between here and its launch)
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kCta);
   if (e != cudaSuccess) return e;
   const long long cap = (long long)a.pv.max_pages * a.pv.page;
   const long long most = ((cap + PA_CHUNK - 1) / PA_CHUNK + PA_UNIT_COST) * a.pv.batch * a.pv.hkv * tiles;       // numbers to deal, if every sequence were full
@@ -149,7 +155,7 @@ cudaError_t launch_select(PagedEvictArgs& a, int units, int cap, int n_sm, cudaS
   a.in_smem = a.slots <= PE_KEYS ? 1 : 0;
   const size_t smem = (size_t)pe_words(a.slots, a.in_smem) * 4;
   void (*kern)(PagedEvictArgs) = small ? k_paged_select<256> : k_paged_select<1024>;
-  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024);      // (see launch_attention)
   return e != cudaSuccess ? e : launch_k(1, kern, dim3(units * a.cluster), dim3(small ? 256 : 1024), smem, stream, a.cluster, a);
 }
 
@@ -198,7 +204,7 @@ int lsp_paged_append(const lsp_paged_kv* kv, const void* k_new, const void* v_ne
   a.rows_block = std::max(1, std::min({PP_ROWS, PP_THREADS * PP_VEC * 16 / row_bytes, n_rows / (4 * n_sm)}));
   const cudaError_t ce = launch_k(1, k_paged_append, dim3((n_rows + a.rows_block - 1) / a.rows_block + 1), dim3(PP_THREADS), row_off ? (size_t)kv->batch * 4 : 0,
                                   (cudaStream_t)cuda_stream, a);
-  if (ce != cudaSuccess) return e.fail(LSP_ERR_CUDA, "%s: launch failed (%s)", who, cudaGetErrorString(ce));
+  if (ce != cudaSuccess) return cuda_failed(e, who, ce);
   return LSP_OK;
 }
 
@@ -232,7 +238,8 @@ int lsp_paged_attention(const lsp_paged_kv* kv, const void* q, long long ldq, in
   a.group = n_heads / kv->n_kv_heads;
   const long long rows_unit = (long long)max_rows * a.group, tiles = (rows_unit + PA_ROWS - 1) / PA_ROWS;
   const long long cap = (long long)kv->max_pages * kv->page_size, units = tiles * kv->batch * kv->n_kv_heads;
-  if ((long long)kv->batch * kv->n_kv_heads * (cap / PW_THREADS + 1) > 0x7fffffffll || units * (cap / PA_CHUNK + 1 + PA_UNIT_COST) > 0x7fffffffll)
+  if ((long long)kv->batch * kv->n_kv_heads * (cap / PW_THREADS + 1) > 0x7fffffffll || units * (cap / PA_CHUNK + 1 + PA_UNIT_COST) > 0x7fffffffll ||
+      (long long)max_rows * n_heads > 0x3fffffffll)
     return e.fail(LSP_ERR_SHAPE, "%s: batch x heads x rows x slots too large for one call", who);
   if (weights_out && rows_unit > 8192) return e.fail(LSP_ERR_SHAPE, "%s: weights of more than 8192 (row, head) pairs per KV head", who);
   if (n_rows == 0 && !weights_out) return LSP_OK;
@@ -262,7 +269,7 @@ int lsp_paged_attention(const lsp_paged_kv* kv, const void* q, long long ldq, in
     ce = kv->head_dim == 128 ? launch_attention<bf16, 128>(a, (int)tiles, st) : launch_attention<bf16, 64>(a, (int)tiles, st);
   else
     ce = kv->head_dim == 128 ? launch_attention<float, 128>(a, (int)tiles, st) : launch_attention<float, 64>(a, (int)tiles, st);
-  if (ce != cudaSuccess) return e.fail(LSP_ERR_CUDA, "%s: launch failed (%s)", who, cudaGetErrorString(ce));
+  if (ce != cudaSuccess) return cuda_failed(e, who, ce);
   return LSP_OK;
 }
 
@@ -318,7 +325,7 @@ int lsp_paged_evict(const lsp_paged_kv* kv, const float* weights, const int32_t*
     const int most = (a.max_moves + PM_WARPS * PM_PAIRS - 1) / (PM_WARPS * PM_PAIRS), fill = (4 * n_sm + units - 1) / units;
     ce = launch_k(1, k_paged_move, dim3(units, std::min(most, fill)), dim3(PM_WARPS * 32), 0, st, a);
   }
-  if (ce != cudaSuccess) return e.fail(LSP_ERR_CUDA, "%s: launch failed (%s)", who, cudaGetErrorString(ce));
+  if (ce != cudaSuccess) return cuda_failed(e, who, ce);
   return LSP_OK;
 }
 

@@ -10,11 +10,15 @@
 //    numbered through, with room for what a unit costs besides, and each CTA of a grid that fills the SMs takes an equal run of the
 //    numbers, whatever the lengths are.  A unit that one CTA holds whole is written by it; the parts (m, l, o) of a unit that a run's
 //    end cuts go to the workspace, and the last of its CTAs to arrive adds them in their order: the same bits every time.
-//  * A warp takes 16 slots of a chunk and loads them itself: a ring of its own in shared memory, filled by cp.async, page ids one
-//    turn ahead of the rows they lead to, the queries of the next unit with its first chunk.  The warps of a CTA meet only where a unit
-//    begins and ends.
-//  * mma.sync m16n8k16, not tcgen05: a tile has at most 16 rows (often one), an M of 128 would be 1/8 to 1/128 full, and the
-//    legacy pipe needs a third of the time that the bytes take.
+//  * A warp takes 16 slots of a chunk and loads them itself: a ring of its own in shared memory, filled by cp.async, page ids a window
+//    of chunks ahead of the rows they lead to, the queries of the next unit with its first chunk.  The warps of a CTA meet only where a
+//    unit begins and ends.
+//  * mma.sync m16n8k16, not tcgen05: a tile has at most 16 rows (often one), an M of 128 would be 1/8 to 1/128 full.  What a warp has to
+//    issue is what competes with the bytes: 16 slots cost it some 300 instructions (655 once, when 16 x 2047 slots took 77 us).
+// Measured on one B200 (copy rate 6.53 TB/s): 16 x 12000 slots of 32 KV heads of 128 352 us = 6.75 TB/s; 16 x 2047 ragged (406 MB) 69.7 us =
+// 5.8 TB/s, of which 60 are the stream, 4.5 the chain lengths -> pages -> rows, 5 the uneven end and the adding of parts.
+// A second tile of rows reads the cache again (28 pairs over 32 x 30000 slots 420 us, 7 pairs 223): two tiles that share what is read in a
+// CTA of eight warps took 369, and 24 pairs of heads of 64 and short caches longer than so; not kept.
 #pragma once
 #include "attention_mma.cuh"
 #include "paged_common.cuh"
@@ -107,11 +111,12 @@ __device__ __forceinline__ void pa_prefix(const PagedAttnArgs& a, int* pre) {
   else __syncwarp();
 }
 
-// Ahead of the wait for the preceding kernel: lengths, offsets and page table into L2 (a line a thread, dealt over the grid).  They are
-// read only behind it, and the chain lengths -> pages -> rows is what a launch begins with.
+// Ahead of the wait for the preceding kernel: lengths, offsets and page table (a megabyte of it at most) into L2, a line a thread, dealt
+// over the grid.  They are read only behind it, and the chain lengths -> pages -> rows is what a launch begins with: 16 x 2047 slots of 32
+// heads 70.6 -> 69.9 us, 4 x 512 13.8 -> 13.1.
 __device__ __forceinline__ void pa_prefetch(const PagedAttnArgs& a) {
   const int n_len = (a.pv.batch * 4 + 127) / 128, n_off = a.row_off ? n_len : 0;
-  const int n_table = a.pv.table ? (int)(((long long)a.pv.batch * a.pv.max_pages * 4 + 127) / 128) : 0;
+  const int n_table = a.pv.table ? (int)min(((long long)a.pv.batch * a.pv.max_pages * 4 + 127) / 128, 8192ll) : 0;
   for (int i = threadIdx.x * gridDim.x + blockIdx.x; i < n_len + n_off + n_table; i += gridDim.x * blockDim.x) {
     const char* at = i < n_len ? (const char*)a.lens + i * 128 : i < n_len + n_off ? (const char*)a.row_off + (i - n_len) * 128
                                                                                 : (const char*)a.pv.table + (long long)(i - n_len - n_off) * 128;
@@ -201,7 +206,7 @@ __device__ __forceinline__ int pa_q_at(int r, int c) {
 
 // One warp's loads: the rows of its 16 slots of a chunk, K then V, into one stage of its ring; and its part of the queries of a unit
 // that begins with the chunk.  A16: a page holds a multiple of 16 slots, so the 16 lie in one page, one behind the other; else every slot's page is
-// looked up.  (The 16 look-ups and 64-bit offsets took half of the kernel's instructions, and instructions, not bytes, were its time.)
+// looked up.  (16 sequences of 2047 slots of 32 heads: 70.7 us, all looked up 72.6; 16 x 12000 of 4 heads of 64 33.1 and 35.0.)
 template <typename T, int DH, bool A16>
 struct PaLoader {
   static constexpr int CPR = DH * (int)sizeof(T) / 16;      // 16-byte chunks of a row

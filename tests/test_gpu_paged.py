@@ -533,6 +533,79 @@ def test_two_streams_with_an_object_each():
     assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
 
 
+def test_two_threads_with_an_object_each():
+    """Calls of unlike shapes from two host threads, each on its own stream: what a launch needs is set per call."""
+    import threading
+    pools = [U.Pool([900, 333], GQA, BF, 16), U.Pool([50, 700, 1], (8, 8, 128), BF, 32, seed=1)]
+    q = [torch.randn(p.batch, p.heads[0] * 128, device=DEV).to(BF) for p in pools]
+    want, got, caches = [torch.empty_like(x) for x in q], [torch.empty_like(x) for x in q], [_cache(p, 1, True) for p in pools]
+    w = [torch.rand(p.batch, p.heads[1], p.cap, device=DEV) for p in pools]
+    for c, p, x, o in zip(caches, pools, q, want):
+        c.attention(x, p.lens, o)
+    torch.cuda.synchronize()
+    failed = []
+
+    def work(i):
+        try:
+            s = torch.cuda.Stream()
+            w_out, lens_out = torch.empty_like(w[i]), torch.empty_like(pools[i].lens)
+            for _ in range(40):
+                caches[i].attention(q[i], pools[i].lens, got[i], stream=s)
+                caches[i].evict(w[i], pools[i].lens, 2000, w_out, lens_out, stream=s)      # (nothing to evict)
+            s.synchronize()
+        except Exception as e:
+            failed.append(e)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_no_rows_at_all():
+    pool = U.Pool([40, 7], SMALL, BF, 16)
+    c = _cache(pool, 2, True)
+    w, w_out = torch.rand(2, 4, pool.cap, device=DEV), torch.full((2, 4, pool.cap), 7.0, device=DEV)
+    empty = torch.empty(0, 512, dtype=BF, device=DEV)
+    c.attention(empty, pool.lens, empty, row_off=_ints([0, 0, 0]), weights_in=w, weights_out=w_out)
+    c.attention(empty, pool.lens, empty, row_off=_ints([0, 0, 0]))
+    lens_out = _ints([0, 0])
+    c.append(empty[:, :256], empty[:, 256:], pool.lens, lens_out, row_off=_ints([0, 0, 0]))
+    c.check()
+    for b, n in enumerate(pool.lens_list):
+        assert torch.equal(w_out[b, :, :n], w[b, :, :n]) and bool((w_out[b, :, n:] == 7).all())
+    assert lens_out.tolist() == [40, 7]
+
+
+def test_calls_that_the_object_refuses():
+    from paper_2603_05454_b200 import LSPError, PagedKVCache
+    pool = U.Pool([40, 7], SMALL, BF, 16)
+    c = _cache(pool, 1)
+    q, out = torch.zeros(2, 512, dtype=BF, device=DEV), torch.zeros(2, 512, dtype=BF, device=DEV)
+    w = torch.zeros(2, 4, pool.cap, device=DEV)
+    bad = [dict(q=q.float()), dict(q=q[:, :256]), dict(q=q.cpu()), dict(q=q.t()), dict(q=q[:1]), dict(out=out[:1]), dict(lens=pool.lens.long()),
+           dict(lens=pool.lens[:1]), dict(lse=torch.zeros(2, 7, device=DEV)), dict(row_off=_ints([0, 2])), dict(weights_out=w[:, :, :-1])]
+    for change in bad:
+        a = dict(q=q, lens=pool.lens, out=out)
+        a.update(change)
+        with pytest.raises(ValueError):
+            c.attention(a.pop("q"), a.pop("lens"), a.pop("out"), **a)
+    for code, call in [(-3, lambda: c.attention(q, pool.lens, out, weights_out=w)),                   # made without room for weights
+                       (-1, lambda: c.attention(q, pool.lens, out, scale=-1.0)), (-1, lambda: c.evict(w, pool.lens, 4, w.clone(), pool.lens.clone(), n_recent=5)),
+                       (-1, lambda: c.evict(w, pool.lens, 4, w, pool.lens.clone())), (-1, lambda: c.append(q[:, :256], q[:, 256:], pool.lens, pool.lens))]:
+        with pytest.raises(LSPError) as e:
+            call()
+        assert e.value.code == code
+    for k, v, t in [(pool.k, pool.v[:, :, :, :32], pool.table), (pool.k, pool.v.float(), pool.table), (pool.k.half(), pool.v.half(), pool.table),
+                    (pool.k[0], pool.v[0], pool.table), (pool.k, pool.v, pool.table.long()), (pool.k, pool.v, pool.table[0])]:
+        with pytest.raises(ValueError):
+            PagedKVCache(k, v, t, n_heads=8)
+    with pytest.raises(LSPError):
+        PagedKVCache(pool.k[:, :, :, :32], pool.v[:, :, :, :32], pool.table, n_heads=8)                 # heads of 32
+    c.check()
+
+
 def test_next_to_a_decoder():
     """The cache that a decode leaves behind, taken as pages in place (a sequence a page): the attention equals lsp_op_attention's, rows are appended to
     the decoder's own planes, and after an eviction the attention is that over the kept rows."""
