@@ -145,18 +145,23 @@ cudaError_t launch_attention(const PagedAttnArgs& a0, int tiles, cudaStream_t st
                   stream, a, key_blocks);
 }
 
-// The selection's launch: 1024 threads a CTA, a cluster of CTAs per unit while that fills no more than the SMs and leaves each CTA 2048 slots
-// (or where a CTA cannot hold them); 256 threads where there are more units than SMs (several fit an SM) and a thread has at most 32 slots.
-cudaError_t launch_select(PagedEvictArgs& a, int units, int cap, int n_sm, cudaStream_t stream) {
+// Where there are more units than SMs, of at most 8192 slots: a CTA of 256 threads each, which moves what it selected.  Else CTAs of 1024 threads, a
+// cluster of them per unit while that fills no more than the SMs and leaves each CTA 2048 slots (or where a CTA cannot hold them), and the
+// moves over the whole grid.
+cudaError_t launch_evict(PagedEvictArgs& a, int units, int cap, int n_sm, cudaStream_t stream) {
   const bool small = units > n_sm && cap <= 8192;
   a.cluster = 1;
-  while (a.cluster < PE_CLUSTER && (cap > PE_SLOTS * a.cluster || (!small && 2 * a.cluster * units <= n_sm && cap / (2 * a.cluster) >= 2048))) a.cluster *= 2;
+  while (!small && a.cluster < PE_CLUSTER && (cap > PE_SLOTS * a.cluster || (2 * a.cluster * units <= n_sm && cap / (2 * a.cluster) >= 2048))) a.cluster *= 2;
   a.slots = ((cap + 31) / 32 + a.cluster - 1) / a.cluster * 32;
   a.in_smem = a.slots <= PE_KEYS ? 1 : 0;
   const size_t smem = (size_t)pe_words(a.slots, a.in_smem) * 4;
-  void (*kern)(PagedEvictArgs) = small ? k_paged_select<256> : k_paged_select<1024>;
-  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024);      // (see launch_attention)
-  return e != cudaSuccess ? e : launch_k(1, kern, dim3(units * a.cluster), dim3(small ? 256 : 1024), smem, stream, a.cluster, a);
+  void (*kern)(PagedEvictArgs) = small ? k_paged_select<256, true> : k_paged_select<1024, false>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024);      // (see launch_attention)
+  if (e == cudaSuccess) e = launch_k(1, kern, dim3(units * a.cluster), dim3(small ? 256 : 1024), smem, stream, a.cluster, a);
+  if (e != cudaSuccess || small || a.max_moves == 0) return e;
+  // as many blocks as are resident at once (four an SM): their warps take pairs in turn
+  const int most = (a.max_moves + PM_WARPS * PM_PAIRS - 1) / (PM_WARPS * PM_PAIRS), fill = (4 * n_sm + units - 1) / units;
+  return launch_k(1, k_paged_move, dim3(units, std::min(most, fill)), dim3(PM_WARPS * 32), 0, stream, a);
 }
 
 }  // namespace
@@ -319,12 +324,7 @@ int lsp_paged_evict(const lsp_paged_kv* kv, const float* weights, const int32_t*
   int dev = 0, n_sm = 0;
   cudaError_t ce = cudaGetDevice(&dev);
   if (ce == cudaSuccess) ce = cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev);
-  if (ce == cudaSuccess) ce = launch_select(a, units, (int)cap, n_sm, st);
-  if (ce == cudaSuccess && a.max_moves > 0) {
-    // as many blocks as are resident at once (four an SM): their warps take pairs in turn
-    const int most = (a.max_moves + PM_WARPS * PM_PAIRS - 1) / (PM_WARPS * PM_PAIRS), fill = (4 * n_sm + units - 1) / units;
-    ce = launch_k(1, k_paged_move, dim3(units, std::min(most, fill)), dim3(PM_WARPS * 32), 0, st, a);
-  }
+  if (ce == cudaSuccess) ce = launch_evict(a, units, (int)cap, n_sm, st);
   if (ce != cudaSuccess) return cuda_failed(e, who, ce);
   return LSP_OK;
 }

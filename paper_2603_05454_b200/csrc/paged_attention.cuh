@@ -111,17 +111,13 @@ __device__ __forceinline__ void pa_prefix(const PagedAttnArgs& a, int* pre) {
   else __syncwarp();
 }
 
-// Ahead of the wait for the preceding kernel: lengths, offsets and page table (a megabyte of it at most) into L2, a line a thread, dealt
-// over the grid.  They are read only behind it, and the chain lengths -> pages -> rows is what a launch begins with: 16 x 2047 slots of 32
-// heads 70.6 -> 69.9 us, 4 x 512 13.8 -> 13.1.
+// Ahead of the wait for the preceding kernel: lengths, offsets and page table into L2.  They are read only behind it, and the chain lengths
+// -> pages -> rows is what a launch begins with: 16 x 2047 slots of 32 heads 70.6 -> 69.9 us, 4 x 512 13.8 -> 13.1.
 __device__ __forceinline__ void pa_prefetch(const PagedAttnArgs& a) {
-  const int n_len = (a.pv.batch * 4 + 127) / 128, n_off = a.row_off ? n_len : 0;
-  const int n_table = a.pv.table ? (int)min(((long long)a.pv.batch * a.pv.max_pages * 4 + 127) / 128, 8192ll) : 0;
-  for (int i = threadIdx.x * gridDim.x + blockIdx.x; i < n_len + n_off + n_table; i += gridDim.x * blockDim.x) {
-    const char* at = i < n_len ? (const char*)a.lens + i * 128 : i < n_len + n_off ? (const char*)a.row_off + (i - n_len) * 128
-                                                                                : (const char*)a.pv.table + (long long)(i - n_len - n_off) * 128;
-    asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
-  }
+  const int i = threadIdx.x * gridDim.x + blockIdx.x, n = gridDim.x * blockDim.x;
+  pg_prefetch(a.lens, a.pv.batch * 4, i, n);
+  pg_prefetch(a.row_off, a.pv.batch * 4, i, n);
+  pg_prefetch_table(a.pv);
 }
 
 // How the numbers are dealt: CTA i of n (those that get at least one) has numbers [run(i), run(i + 1)), run(i) = floor(total i / n).

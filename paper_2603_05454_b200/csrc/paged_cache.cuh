@@ -220,7 +220,67 @@ __device__ __forceinline__ uint4 ld_cluster_u4(uint32_t addr) {
 // Shared memory of a selection, in words: counts, bitmap, holes and movers ahead of each of its words, keys.
 __host__ __device__ inline int pe_words(int slots, int in_smem) { return 2 * PE_BINS + slots / 32 * 3 + 4 + (in_smem ? slots : 0); }
 
-template <int THREADS>
+// What moves of a unit, the pairs (source[i], target[i]): weight, position and rows, by n_warps warps, this one the w-th.  A warp takes PM_PAIRS
+// pairs at a time; the K row in the first half of the lanes, the V row in the second (rows of 512 bytes in two turns).  A turn's rows are under
+// way while the next one's pages, and the slots of the one behind it, are looked up: without that the chain of the reads is what a warp waits
+// for.
+__device__ __forceinline__ void pe_move(const PagedEvictArgs& a, int unit, const int* source, const int* target, int n, int w, int n_warps) {
+  const int b = unit / a.pv.hkv, kvh = unit % a.pv.hkv, lane = threadIdx.x & 31;
+  const int* list = lane < PM_PAIRS ? source : target;      // lanes 0 .. 3: sources, lanes 4 .. 7: targets
+  const int step = n_warps * PM_PAIRS;
+  int i0 = w * PM_PAIRS;
+  if (i0 >= n) return;
+  const long long base = (long long)unit * pg_capacity(a.pv);
+  auto slot = [&](int i) { i += lane % PM_PAIRS; return lane < 2 * PM_PAIRS && i < n ? list[i] : -1; };
+  auto offset = [&](int j) -> long long {
+    const int id = j >= 0 ? pg_page(a.pv, b, j) : -1;
+    return id < 0 ? -1 : ((long long)id * a.pv.page_stride + (long long)(j % a.pv.page) * a.pv.row_stride + (long long)kvh * a.pv.head_stride) * a.esz;
+  };
+  int j = slot(i0), j2 = slot(i0 + step);
+  long long off = offset(j);
+  char* pool = lane < 16 ? a.pv.k : a.pv.v;
+  for (; i0 < n; i0 += step) {
+    const int to_slot = __shfl_down_sync(0xffffffffu, j, PM_PAIRS);
+    long long from[PM_PAIRS], to[PM_PAIRS];
+#pragma unroll
+    for (int i = 0; i < PM_PAIRS; ++i) {
+      from[i] = __shfl_sync(0xffffffffu, off, i);
+      to[i] = __shfl_sync(0xffffffffu, off, PM_PAIRS + i);
+      if (from[i] < 0) to[i] = -1;
+    }
+    const int c0 = (lane & 15) * 16;
+    uint4 x[PM_PAIRS];
+#pragma unroll
+    for (int i = 0; i < PM_PAIRS; ++i)
+      if (to[i] >= 0 && c0 < a.head_bytes) x[i] = *reinterpret_cast<const uint4*>(pool + from[i] + c0);
+    const bool mine = lane < PM_PAIRS && j >= 0;
+    const float weight = mine ? a.weights[base + j] : 0.f;
+    const int p = mine && a.pos ? a.pos[base + j] : j;
+    const int j3 = slot(i0 + 2 * step);
+    const long long off2 = offset(j2);
+#pragma unroll
+    for (int i = 0; i < PM_PAIRS; ++i)
+      if (to[i] >= 0 && c0 < a.head_bytes) *reinterpret_cast<uint4*>(pool + to[i] + c0) = x[i];
+    if (c0 + 256 < a.head_bytes) {
+#pragma unroll
+      for (int i = 0; i < PM_PAIRS; ++i)
+        if (to[i] >= 0) x[i] = *reinterpret_cast<const uint4*>(pool + from[i] + c0 + 256);
+#pragma unroll
+      for (int i = 0; i < PM_PAIRS; ++i)
+        if (to[i] >= 0) *reinterpret_cast<uint4*>(pool + to[i] + c0 + 256) = x[i];
+    }
+    if (mine) {
+      a.weights_out[base + to_slot] = weight;
+      if (a.pos_out) a.pos_out[base + to_slot] = p;
+    }
+    j = j2;
+    j2 = j3;
+    off = off2;
+  }
+}
+
+// MOVE: the CTA moves what it selected (one CTA a unit); else k_paged_move does.
+template <int THREADS, bool MOVE>
 __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a) {
   extern __shared__ __align__(16) unsigned pe_smem[];
   unsigned* keys = pe_smem + 2 * PE_BINS;          // behind two sets of counts: [slots], if they are kept here
@@ -232,12 +292,21 @@ __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a
   __shared__ unsigned warp_or[32];
   __shared__ int groups_of[2][PE_BINS / 64];
   int turn = 0;
-  const int CL = a.cluster, rank = CL > 1 ? (int)cluster_ctarank() : 0, tid = threadIdx.x, lane = tid & 31;
+  const int CL = MOVE ? 1 : a.cluster, rank = CL > 1 ? (int)cluster_ctarank() : 0, tid = threadIdx.x, lane = tid & 31;
   auto barrier = [&]() { if (CL > 1) cluster_sync(); else __syncthreads(); };
-  pdl_begin();
   const int unit = blockIdx.x / CL, b = unit / a.pv.hkv, cap = pg_capacity(a.pv);
-  const int n = pg_len(a.pv, a.lens[b]);
   const long long base = (long long)unit * cap;
+  pdl_release();
+  {
+    // (a sequence to thin has more slots than the budget; of the others fewer are read)
+    const long long bytes = (long long)min(cap, a.budget) * 4;
+    pg_prefetch(a.lens, a.pv.batch * 4, tid + blockIdx.x * THREADS, gridDim.x * THREADS);
+    pg_prefetch(a.weights + base, bytes, tid + rank * THREADS, CL * THREADS);
+    if (a.pos) pg_prefetch(a.pos + base, bytes, tid + rank * THREADS, CL * THREADS);
+    pg_prefetch_table(a.pv);
+  }
+  pdl_wait();
+  const int n = pg_len(a.pv, a.lens[b]);
   int* moves = a.moves + (long long)unit * (1 + 2 * (long long)a.max_moves);
   if (unit % a.pv.hkv == 0 && rank == 0 && tid == 0) a.lens_out[b] = min(n, a.budget);
   // this CTA's slots: [s0, s0 + ns)
@@ -248,7 +317,7 @@ __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a
   int* pos_out = a.pos_out ? a.pos_out + base + s0 : nullptr;
   auto pos_of = [&](int j) { return pos ? pos[j] : s0 + j; };
   if (n <= a.budget) {
-    if (rank == 0 && tid == 0) moves[0] = 0;
+    if (!MOVE && rank == 0 && tid == 0) moves[0] = 0;
     for (int j = tid; j < ns; j += THREADS) {
       weights_out[j] = weights[j];
       if (pos_out) pos_out[j] = pos_of(j);
@@ -417,7 +486,7 @@ __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a
     at.y += __popc(bits[w] & ~ahead(w));
   }
   __syncthreads();
-  if (rank == 0 && tid == 0) moves[0] = movers;
+  if (!MOVE && rank == 0 && tid == 0) moves[0] = movers;
   int* src = moves + 1;
   int* dst = src + a.max_moves;
   const unsigned lower = (1u << lane) - 1;
@@ -448,66 +517,17 @@ __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a
     }
   }
   if (CL > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+  if (MOVE) {
+    __syncthreads();
+    pe_move(a, unit, src, dst, movers, tid >> 5, THREADS / 32);
+  }
 }
 
-// What moves: weight, position and rows.  A warp takes PM_PAIRS pairs of slots at a time; the K row in the first half of the lanes, the V row in
-// the second (rows of 512 bytes in two turns).  A turn's rows are under way while the next one's pages, and the slots of the one behind it,
-// are looked up: without that the chain of the four reads is what a warp waits for.
+// The moves of all units: blocks (unit, y).
 __global__ void __launch_bounds__(PM_WARPS * 32) k_paged_move(const PagedEvictArgs a) {
   pdl_begin();
-  const int unit = blockIdx.x, b = unit / a.pv.hkv, kvh = unit % a.pv.hkv, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const int* moves = a.moves + (long long)unit * (1 + 2 * (long long)a.max_moves);
-  const int* list = moves + 1 + (lane < PM_PAIRS ? 0 : a.max_moves);      // lanes 0 .. 3: sources, lanes 4 .. 7: targets
-  const int n = moves[0], step = gridDim.y * PM_WARPS * PM_PAIRS;
-  int i0 = (blockIdx.y * PM_WARPS + w) * PM_PAIRS;
-  if (i0 >= n) return;
-  const long long base = (long long)unit * pg_capacity(a.pv);
-  auto slot = [&](int i) { i += lane % PM_PAIRS; return lane < 2 * PM_PAIRS && i < n ? list[i] : -1; };
-  auto offset = [&](int j) -> long long {
-    const int id = j >= 0 ? pg_page(a.pv, b, j) : -1;
-    return id < 0 ? -1 : ((long long)id * a.pv.page_stride + (long long)(j % a.pv.page) * a.pv.row_stride + (long long)kvh * a.pv.head_stride) * a.esz;
-  };
-  int j = slot(i0), j2 = slot(i0 + step);
-  long long off = offset(j);
-  char* pool = lane < 16 ? a.pv.k : a.pv.v;
-  for (; i0 < n; i0 += step) {
-    const int target = __shfl_down_sync(0xffffffffu, j, PM_PAIRS);
-    long long from[PM_PAIRS], to[PM_PAIRS];
-#pragma unroll
-    for (int i = 0; i < PM_PAIRS; ++i) {
-      from[i] = __shfl_sync(0xffffffffu, off, i);
-      to[i] = __shfl_sync(0xffffffffu, off, PM_PAIRS + i);
-      if (from[i] < 0) to[i] = -1;
-    }
-    const int c0 = (lane & 15) * 16;
-    uint4 x[PM_PAIRS];
-#pragma unroll
-    for (int i = 0; i < PM_PAIRS; ++i)
-      if (to[i] >= 0 && c0 < a.head_bytes) x[i] = *reinterpret_cast<const uint4*>(pool + from[i] + c0);
-    const bool mine = lane < PM_PAIRS && j >= 0;
-    const float weight = mine ? a.weights[base + j] : 0.f;
-    const int p = mine && a.pos ? a.pos[base + j] : j;
-    const int j3 = slot(i0 + 2 * step);
-    const long long off2 = offset(j2);
-#pragma unroll
-    for (int i = 0; i < PM_PAIRS; ++i)
-      if (to[i] >= 0 && c0 < a.head_bytes) *reinterpret_cast<uint4*>(pool + to[i] + c0) = x[i];
-    if (c0 + 256 < a.head_bytes) {
-#pragma unroll
-      for (int i = 0; i < PM_PAIRS; ++i)
-        if (to[i] >= 0) x[i] = *reinterpret_cast<const uint4*>(pool + from[i] + c0 + 256);
-#pragma unroll
-      for (int i = 0; i < PM_PAIRS; ++i)
-        if (to[i] >= 0) *reinterpret_cast<uint4*>(pool + to[i] + c0 + 256) = x[i];
-    }
-    if (mine) {
-      a.weights_out[base + target] = weight;
-      if (a.pos_out) a.pos_out[base + target] = p;
-    }
-    j = j2;
-    j2 = j3;
-    off = off2;
-  }
+  const int* moves = a.moves + (long long)blockIdx.x * (1 + 2 * (long long)a.max_moves);
+  pe_move(a, blockIdx.x, moves + 1, moves + 1 + a.max_moves, moves[0], blockIdx.y * PM_WARPS + (threadIdx.x >> 5), gridDim.y * PM_WARPS);
 }
 
 }  // namespace lsp

@@ -40,6 +40,14 @@ __device__ __forceinline__ int pg_page(const PagedView& pv, int b, int j) {
   }
   return id;
 }
+// Asks for bytes at p to come to L2 (thread `i` of n, a line each).  Ahead of the wait for a preceding kernel: nothing is read.
+__device__ __forceinline__ void pg_prefetch(const void* p, long long bytes, int i, int n) {
+  for (long long at = (long long)i * 128; p && at < bytes; at += (long long)n * 128) asm volatile("prefetch.global.L2 [%0];" ::"l"((const char*)p + at));
+}
+// The page table, a megabyte of it at most, by the whole grid.
+__device__ __forceinline__ void pg_prefetch_table(const PagedView& pv) {
+  pg_prefetch(pv.table, min((long long)pv.batch * pv.max_pages * 4, 1ll << 20), threadIdx.x * gridDim.x + blockIdx.x, gridDim.x * blockDim.x);
+}
 // Packed rows of sequence b: first one and count (0 with the flag set where the offsets leave the caller's rows).
 struct RowSpan { int first, n; };
 __device__ __forceinline__ RowSpan pg_rows(const PagedView& pv, const int* row_off, int b, int max_rows, int n_rows) {
