@@ -209,7 +209,7 @@ int lsp_paged_append(const lsp_paged_kv* kv, const void* k_new, const void* v_ne
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return e.fail(LSP_ERR_CUDA, "%s: no usable current device", who);
   a.rows_block = std::max(1, std::min({PP_ROWS, PP_THREADS * PP_VEC * 16 / row_bytes, n_rows / (4 * n_sm)}));
-  const cudaError_t ce = launch_k(1, k_paged_append, dim3((n_rows + a.rows_block - 1) / a.rows_block + 1), dim3(PP_THREADS), row_off ? (size_t)kv->batch * 4 : 0,
+  const cudaError_t ce = launch_k(1, k_paged_append, dim3((n_rows + a.rows_block - 1) / a.rows_block + 1), dim3(PP_THREADS), row_off ? (size_t)kv->batch * 8 : 0,
                                   (cudaStream_t)cuda_stream, a);
   if (ce != cudaSuccess) return cuda_failed(e, who, ce);
   return LSP_OK;

@@ -28,11 +28,14 @@ struct PagedAppendArgs {
 
 // Blocks ahead of the last: rows_block packed rows each.  The last block: the lengths.
 __global__ void __launch_bounds__(PP_THREADS) k_paged_append(const PagedAppendArgs a) {
-  extern __shared__ int offsets[];      // [batch] row_off
+  extern __shared__ int offsets[];      // [batch] row_off, [batch] lens (with offsets: a row's sequence is searched for)
   __shared__ int seqs[PP_ROWS], slots[PP_ROWS], poss[PP_ROWS];
   __shared__ long long places[PP_ROWS]; // bytes, -1: nowhere
-  pdl_begin();
   const int B = a.pv.batch, cap = pg_capacity(a.pv);
+  pdl_release();
+  pg_prefetch_table(a.pv);
+  pg_prefetch(a.lens, B * 4, threadIdx.x * gridDim.x + blockIdx.x, gridDim.x * PP_THREADS);
+  pdl_wait();
   if (blockIdx.x == gridDim.x - 1) {
     for (int b = threadIdx.x; b < B; b += PP_THREADS) {
       const RowSpan rs = pg_rows(a.pv, a.row_off, b, a.max_rows, a.n_rows);
@@ -70,7 +73,10 @@ __global__ void __launch_bounds__(PP_THREADS) k_paged_append(const PagedAppendAr
     if (c < total) x[i] = load(c);
   }
   if (a.row_off) {
-    for (int b = threadIdx.x; b < B; b += PP_THREADS) offsets[b] = a.row_off[b];
+    for (int b = threadIdx.x; b < B; b += PP_THREADS) {
+      offsets[b] = a.row_off[b];
+      offsets[B + b] = a.lens[b];
+    }
     __syncthreads();
   }
   if (threadIdx.x < n) {
@@ -89,7 +95,7 @@ __global__ void __launch_bounds__(PP_THREADS) k_paged_append(const PagedAppendAr
     }
     if (b >= 0) {
       const RowSpan rs = pg_rows(a.pv, a.row_off, b, a.max_rows, a.n_rows);
-      const int len = pg_len(a.pv, a.lens[b]), i = r - rs.first;
+      const int len = pg_len(a.pv, a.row_off ? offsets[B + b] : a.lens[b]), i = r - rs.first;
       if (i >= 0 && i < rs.n && len + i < cap) {
         slot = len + i;
         const int id = pg_page(a.pv, b, slot);
