@@ -246,7 +246,7 @@ int lsp_paged_attention(const lsp_paged_kv* kv, const void* q, long long ldq, in
   const long long rows_unit = (long long)max_rows * a.group, tiles = (rows_unit + PA_ROWS - 1) / PA_ROWS;
   const long long cap = (long long)kv->max_pages * kv->page_size, units = tiles * kv->batch * kv->n_kv_heads;
   if ((long long)kv->batch * kv->n_kv_heads * (cap / PW_THREADS + 1) > 0x7fffffffll || units * (cap / PA_CHUNK + 1 + PA_UNIT_COST) > 0x7fffffffll ||
-      (long long)max_rows * n_heads > 0x3fffffffll)
+      (long long)max_rows * n_heads > 0x3fffffffll || max_rows > (1 << 20) || tiles * kv->n_kv_heads > (1 << 20))
     return e.fail(LSP_ERR_SHAPE, "%s: batch x heads x rows x slots too large for one call", who);
   if (weights_out && rows_unit > 8192) return e.fail(LSP_ERR_SHAPE, "%s: weights of more than 8192 (row, head) pairs per KV head", who);
   if (n_rows == 0 && !weights_out) return LSP_OK;

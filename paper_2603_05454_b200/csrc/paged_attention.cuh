@@ -129,7 +129,7 @@ struct PaDeal {
       r = total - q * n;
     }
   }
-  __device__ __forceinline__ int run(int i) const { return i * q + i * r / n; }
+  __device__ __forceinline__ int run(int i) const { return i * q + pg_div(i * r, n); }
   // the CTA whose run holds number c (the estimate is off by one at most: 2^-24 of at most 1024, and the runs' rounding)
   __device__ __forceinline__ int owner(int c) const {
     int i = min(n - 1, (int)((float)c / (float)total * (float)n));
@@ -159,11 +159,12 @@ __device__ __forceinline__ PaPlace pa_place(const PagedAttnArgs& a, const int* p
     const int n = a.lens[lo], cap = pg_capacity(a.pv);
     p.len = n > cap ? cap : n;
     p.chunks = pa_chunks(p.len);
-    const int span = p.chunks + PA_UNIT_COST, tiles = (pre[lo + 1] - pre[lo]) / (span * a.pv.hkv);
-    const int u = (c - pre[lo]) / span;
+    // (quotients: a sequence's KV heads times tiles, at most 2^20 by the call's limits)
+    const int span = p.chunks + PA_UNIT_COST, tiles = pg_div(pre[lo + 1] - pre[lo], span * a.pv.hkv);
+    const int u = pg_div(c - pre[lo], span);
     p.u0 = pre[lo] + u * span;
     p.chunk = c - p.u0;
-    p.kvh = u / tiles;
+    p.kvh = pg_div(u, tiles);
     p.rt = u - p.kvh * tiles;
     if (p.chunk < p.chunks) {
       p.left = min(p.chunks - p.chunk, hi - c);
@@ -174,12 +175,20 @@ __device__ __forceinline__ PaPlace pa_place(const PagedAttnArgs& a, const int* p
   return p;
 }
 
+// A part of a cut unit, noted until the run's end: the unit, and CTAs first .. last, which have a part each; the first one's is its second
+// part where the unit begins in its run.
+struct PaCut {
+  PaPlace p;
+  int first, last, second;
+};
+
 // Where a (row, head) pair of a unit lies: packed row and query head; false behind the sequence's last row.
 __device__ __forceinline__ bool pa_row(const PagedAttnArgs& a, const RowSpan& rs, const PaPlace& p, int i, int& row, int& head) {
   const int x = p.rt * PA_ROWS + i;
   if (x >= rs.n * a.group) return false;
-  row = rs.first + x / a.group;
-  head = p.kvh * a.group + x % a.group;
+  const int r = pg_div(x, a.group);
+  row = rs.first + r;
+  head = p.kvh * a.group + x - r * a.group;
   return true;
 }
 
@@ -224,8 +233,9 @@ struct PaLoader {
   __device__ __forceinline__ void ask(int chunk, int& page, int& row) const {
     const int j = A16 ? (chunk + lane) * PA_CHUNK + w * 16 : (chunk + (lane >> 4)) * PA_CHUNK + w * 16 + (lane & 15);
     const int end = A16 ? min(p.len, (p.chunk + p.left) * PA_CHUNK) : p.len;      // (no pages of chunks that are another CTA's)
-    page = j < end ? pg_page(a.pv, p.b, j) : -1;
-    row = j % a.pv.page;
+    const int n = pg_div(j, a.pv.page);
+    page = j < end ? pg_page(a.pv, p.b, n) : -1;
+    row = j - n * a.pv.page;
   }
   __device__ __forceinline__ void begin() {
     base = p.chunk;
@@ -378,7 +388,7 @@ __device__ __forceinline__ void pa_write_row(const PagedAttnArgs& a, int row, in
 // rows i .. i + n - 1 ([n][DH], pairs of elements exchanged by 4 (row & 3)) and their (m, l); warp w adds row i + w.  A part of a cut unit
 // is noted in cut[] (at most one that begins ahead of the run and one that ends behind it).
 template <typename T, int DH, typename Put>
-__device__ __forceinline__ void pa_finish(const PagedAttnArgs& a, const PaPlace& p, const RowSpan& rs, int lo, PaPlace* cut, char* smem, Put put) {
+__device__ __forceinline__ void pa_finish(const PagedAttnArgs& a, const PaDeal& deal, const PaPlace& p, const RowSpan& rs, int lo, PaCut* cut, char* smem, Put put) {
   constexpr int VEC = DH / 32;
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   float* merge = reinterpret_cast<float*>(smem + PaSmem<T, DH>::merge(a.q_rows));
@@ -386,7 +396,10 @@ __device__ __forceinline__ void pa_finish(const PagedAttnArgs& a, const PaPlace&
   const int n_real = min(PA_ROWS, rs.n * a.group - p.rt * PA_ROWS);
   const bool whole = p.left == p.chunks;
   const int second = lo >= p.u0 ? 0 : 1, part = 2 * blockIdx.x + second;
-  if (!whole && threadIdx.x == 0) cut[second] = p;
+  if (!whole && threadIdx.x == PA_THREADS - 1) {      // (the last warp adds rows last, if any)
+    const int first = deal.owner(p.u0);
+    cut[second] = PaCut{p, first, deal.owner(p.u0 + p.chunks - 1), deal.run(first) < p.u0 ? 1 : 0};
+  }
   for (int i = 0; i < n_real; i += a.merge_rows) {
     if (i > 0) __syncthreads();
     put(i, a.merge_rows, merge + w * a.merge_rows * DH, ml + w * a.merge_rows);
@@ -428,45 +441,43 @@ __device__ __forceinline__ void pa_finish(const PagedAttnArgs& a, const PaPlace&
 // row at a time, 32 parts' (m, l) on its lanes and PA_AHEAD parts' o under way; the code is short because it is fetched cold.
 constexpr int PA_AHEAD = 16;
 template <typename T, int DH>
-__device__ __forceinline__ void pa_join(const PagedAttnArgs& a, const PaDeal& deal, const PaPlace* cut) {
+__device__ __forceinline__ void pa_join(const PagedAttnArgs& a, const PaCut* cut) {
   constexpr int VEC = DH / 32;
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  __shared__ int parts[2][3];                      // of the unit that is this CTA's to add: first CTA and its part, last CTA
+  __shared__ int mine[2];                          // a unit is this CTA's to add
   cp_async_wait<0>();
   __syncthreads();
   if (threadIdx.x < 2) {
-    const PaPlace& p = cut[threadIdx.x];
-    int i0 = 0, i1 = -1, second = 0;
-    if (p.left > 0) {
-      i0 = deal.owner(p.u0);                       // CTAs i0 .. i1 have a part each
-      i1 = deal.owner(p.u0 + p.chunks - 1);
-      second = deal.run(i0) < p.u0 ? 1 : 0;        // the unit begins in the first one's run: its second part
+    const PaCut& c = cut[threadIdx.x];
+    bool last = false;
+    if (c.p.left > 0) {
       __threadfence();
-      if (atomicAdd(a.arrived + i0, 1u) == (unsigned)(i1 - i0)) a.arrived[i0] = 0;
-      else i1 = -1;
+      last = atomicAdd(a.arrived + c.first, 1u) == (unsigned)(c.last - c.first);
+      if (last) a.arrived[c.first] = 0;
       __threadfence();
     }
-    parts[threadIdx.x][0] = i0;
-    parts[threadIdx.x][1] = second;
-    parts[threadIdx.x][2] = i1;
+    mine[threadIdx.x] = last;
   }
   __syncthreads();
+  // the rows of both units dealt to the warps
+  int skip = w;
 #pragma unroll 1
   for (int which = 0; which < 2; ++which) {
-    const int i0 = parts[which][0], n = parts[which][2] - i0 + 1;
-    if (n <= 0) continue;
-    const PaPlace p = cut[which];
+    if (!mine[which]) continue;
+    const PaPlace p = cut[which].p;
+    const int i0 = cut[which].first, second = cut[which].second, n = cut[which].last - i0 + 1;
     const RowSpan rs = pg_rows(a.pv, a.row_off, p.b, a.max_rows, a.n_rows);
     const int n_real = min(PA_ROWS, rs.n * a.group - p.rt * PA_ROWS);
+    int r = skip;
 #pragma unroll 1
-    for (int r = w; r < n_real; r += PA_WARPS) {
+    for (; r < n_real; r += PA_WARPS) {
       float m = -INFINITY, l = 0.f, o[VEC];
 #pragma unroll
       for (int e = 0; e < VEC; ++e) o[e] = 0.f;
 #pragma unroll 1
       for (int k0 = 0; k0 < n; k0 += 32) {
         const int k = min(k0 + lane, n - 1);
-        const int slot = (2 * (i0 + k) + (k == 0 ? parts[which][1] : 0)) * PA_ROWS + r;
+        const int slot = (2 * (i0 + k) + (k == 0 ? second : 0)) * PA_ROWS + r;
         const float2 x = __ldcg(a.part_ml + slot);
         float y[PA_AHEAD][VEC], f = 0.f;
 #pragma unroll 1
@@ -502,6 +513,7 @@ __device__ __forceinline__ void pa_join(const PagedAttnArgs& a, const PaDeal& de
       pa_row(a, rs, p, r, row, head);
       pa_write_row<T, DH>(a, row, head, o, m, l);
     }
+    skip = r - n_real;
   }
 }
 
@@ -538,8 +550,8 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 2)) k_paged_attn_mm
   const int lo = deal.run(blockIdx.x), hi = deal.run(blockIdx.x + 1);
   PaPlace p = pa_place(a, pre, lo, hi);
   if (p.left == 0) return;
-  __shared__ PaPlace cut[2];
-  if (threadIdx.x < 2) cut[threadIdx.x].left = 0;
+  __shared__ PaCut cut[2];
+  if (threadIdx.x < 2) cut[threadIdx.x].p.left = 0;
 
   PaRing<bf16, DH, A16> ring(a, pre, hi, p, pa_smem);
   // this lane's rows and chunks of the K and V tiles (ldmatrix); chunk c lies at c ^ (row & 7): further chunks are the same address with
@@ -662,7 +674,7 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 2)) k_paged_attn_mm
       l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
       m[h] *= a.scale_log2;
     }
-    pa_finish<bf16, DH>(a, p, rs, lo, cut, pa_smem, [&](int i0, int n, float* dst, float2* ml) {
+    pa_finish<bf16, DH>(a, deal, p, rs, lo, cut, pa_smem, [&](int i0, int n, float* dst, float2* ml) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int r = g + 8 * h - i0;
@@ -673,7 +685,7 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 2)) k_paged_attn_mm
       }
     });
   }
-  pa_join<bf16, DH>(a, deal, cut);
+  pa_join<bf16, DH>(a, cut);
 }
 
 // ---- fp32: CUDA cores ----------------------------------------------------------------------------------------------------
@@ -696,8 +708,8 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 4)) k_paged_attn_si
   const int lo = deal.run(blockIdx.x), hi = deal.run(blockIdx.x + 1);
   PaPlace p = pa_place(a, pre, lo, hi);
   if (p.left == 0) return;
-  __shared__ PaPlace cut[2];
-  if (threadIdx.x < 2) cut[threadIdx.x].left = 0;
+  __shared__ PaCut cut[2];
+  if (threadIdx.x < 2) cut[threadIdx.x].p.left = 0;
 
   PaRing<float, DH, A16> ring(a, pre, hi, p, pa_smem);
   const int key = lane & 15, half = lane >> 4;
@@ -778,7 +790,7 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 4)) k_paged_attn_si
     }
 #pragma unroll
     for (int r = 0; r < NR; ++r) l[r] = warp_sum(half == 0 ? l[r] : 0.f);
-    pa_finish<float, DH>(a, p, rs, lo, cut, pa_smem, [&](int i0, int n, float* dst, float2* ml) {
+    pa_finish<float, DH>(a, deal, p, rs, lo, cut, pa_smem, [&](int i0, int n, float* dst, float2* ml) {
 #pragma unroll
       for (int r = 0; r < NR; ++r) {
         const int i = r - i0;
@@ -789,7 +801,7 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 4)) k_paged_attn_si
       }
     });
   }
-  pa_join<float, DH>(a, deal, cut);
+  pa_join<float, DH>(a, cut);
 }
 
 // ---- gathered weights ----------------------------------------------------------------------------------------------------

@@ -98,8 +98,8 @@ __global__ void __launch_bounds__(PP_THREADS) k_paged_append(const PagedAppendAr
       const int len = pg_len(a.pv, a.row_off ? offsets[B + b] : a.lens[b]), i = r - rs.first;
       if (i >= 0 && i < rs.n && len + i < cap) {
         slot = len + i;
-        const int id = pg_page(a.pv, b, slot);
-        if (id >= 0) place = ((long long)id * a.pv.page_stride + (long long)(slot % a.pv.page) * a.pv.row_stride) * a.esz;
+        place = pg_slot(a.pv, b, slot);
+        if (place >= 0) place *= a.esz;
         position = a.seen ? a.seen[b] + i : slot;
       }
     }
@@ -236,11 +236,16 @@ __device__ __forceinline__ void pe_move(const PagedEvictArgs& a, int unit, const
   const int step = n_warps * PM_PAIRS;
   int i0 = w * PM_PAIRS;
   if (i0 >= n) return;
-  const long long base = (long long)unit * pg_capacity(a.pv);
-  auto slot = [&](int i) { i += lane % PM_PAIRS; return lane < 2 * PM_PAIRS && i < n ? list[i] : -1; };
+  const int cap = pg_capacity(a.pv);
+  auto slot = [&](int i) {
+    i += lane % PM_PAIRS;
+    const int j = lane < 2 * PM_PAIRS && i < n ? list[i] : -1;
+    return j < cap ? j : -1;
+  };
+  const long long base = (long long)unit * cap;
   auto offset = [&](int j) -> long long {
-    const int id = j >= 0 ? pg_page(a.pv, b, j) : -1;
-    return id < 0 ? -1 : ((long long)id * a.pv.page_stride + (long long)(j % a.pv.page) * a.pv.row_stride + (long long)kvh * a.pv.head_stride) * a.esz;
+    const long long at = j >= 0 ? pg_slot(a.pv, b, j) : -1;
+    return at < 0 ? -1 : (at + (long long)kvh * a.pv.head_stride) * a.esz;
   };
   int j = slot(i0), j2 = slot(i0 + step);
   long long off = offset(j);
@@ -259,7 +264,7 @@ __device__ __forceinline__ void pe_move(const PagedEvictArgs& a, int unit, const
 #pragma unroll
     for (int i = 0; i < PM_PAIRS; ++i)
       if (to[i] >= 0 && c0 < a.head_bytes) x[i] = *reinterpret_cast<const uint4*>(pool + from[i] + c0);
-    const bool mine = lane < PM_PAIRS && j >= 0;
+    const bool mine = lane < PM_PAIRS && j >= 0 && to_slot >= 0;
     const float weight = mine ? a.weights[base + j] : 0.f;
     const int p = mine && a.pos ? a.pos[base + j] : j;
     const int j3 = slot(i0 + 2 * step);
@@ -383,7 +388,7 @@ __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a
           for (int r = 0; r < PE_CLUSTER; ++r) x += y[r];
         }
         int up = pe_warp_sum_before(x) + x;
-        const int g = __ffs(__ballot_sync(0xffffffffu, want <= up)) - 1, base_g = __shfl_sync(0xffffffffu, up - x, g);
+        const int g = __ffs(__ballot_sync(0xffffffffu, want <= up) | 0x80000000u) - 1, base_g = __shfl_sync(0xffffffffu, up - x, g);
         int2 h = make_int2(0, 0);
         const unsigned* mine = hist + g * 64 + lane * 2;
         if (CL == 1) {
@@ -399,7 +404,7 @@ __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a
           }
         }
         up = base_g + pe_warp_sum_before(h.x + h.y) + h.x + h.y;
-        const int l = __ffs(__ballot_sync(0xffffffffu, want <= up)) - 1;
+        const int l = __ffs(__ballot_sync(0xffffffffu, want <= up) | 0x80000000u) - 1;
         if (lane == l) {
           const int before = up - h.x - h.y;
           const bool second = want > before + h.x;
@@ -463,7 +468,7 @@ __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a
     count.y += __popc(bits[w] & ~ahead(w));
   }
   int2 at = pe_sums_before<THREADS>(count, warp_sums, all);
-  int movers = all.y;
+  int holes = all.x, movers = all.y;                 // (as many, and at most max_moves, unless the inputs change underneath)
   if (CL > 1) {
     if (tid == 0) {
       shared_counts[0] = all.x;
@@ -474,12 +479,13 @@ __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a
 #pragma unroll
     for (int r = 0; r < PE_CLUSTER; ++r)
       if (r < CL) x[r] = ld_cluster_u4(cluster_map(smem_u32(shared_counts), r));
-    movers = 0;
+    holes = movers = 0;
 #pragma unroll
     for (int r = 0; r < PE_CLUSTER; ++r)
       if (r < CL) {
         at.x += r < rank ? (int)x[r].x : 0;
         at.y += r < rank ? (int)x[r].y : 0;
+        holes += (int)x[r].x;
         movers += (int)x[r].y;
       }
     // Nobody leaves while another reads its counts; that orders no memory, and an arrival with release would wait for the stores below.
@@ -492,7 +498,8 @@ __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a
     at.y += __popc(bits[w] & ~ahead(w));
   }
   __syncthreads();
-  if (!MOVE && rank == 0 && tid == 0) moves[0] = movers;
+  const int n_moves = min(min(holes, movers), a.max_moves);
+  if (!MOVE && rank == 0 && tid == 0) moves[0] = n_moves;
   int* src = moves + 1;
   int* dst = src + a.max_moves;
   const unsigned lower = (1u << lane) - 1;
@@ -518,14 +525,16 @@ __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a
         weights_out[j] = weight[i];
         if (pos_out) pos_out[j] = p[i];
       }
-      if (is_front && !is_kept) dst[holes_at[w] + __popc(~m & front & lower)] = s0 + j;
-      if (!is_front && is_kept) src[movers_at[w] + __popc(m & ~front & lower)] = s0 + j;
+      if (is_front != is_kept) {                     // a freed one ahead, a kept one behind
+        const int i = is_front ? holes_at[w] + __popc(~m & front & lower) : movers_at[w] + __popc(m & ~front & lower);
+        if (i < a.max_moves) (is_front ? dst : src)[i] = s0 + j;
+      }
     }
   }
   if (CL > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
   if (MOVE) {
     __syncthreads();
-    pe_move(a, unit, src, dst, movers, tid >> 5, THREADS / 32);
+    pe_move(a, unit, src, dst, n_moves, tid >> 5, THREADS / 32);
   }
 }
 
