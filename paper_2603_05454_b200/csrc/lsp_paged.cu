@@ -145,20 +145,20 @@ cudaError_t launch_attention(const PagedAttnArgs& a0, int tiles, cudaStream_t st
                   stream, a, key_blocks);
 }
 
-// Where there are more units than SMs, of at most 8192 slots: a CTA of 256 threads each, which moves what it selected.  Else CTAs of 1024 threads, a
+// Where there are more units than SMs, of at most 4096 slots: a CTA of 256 threads each (four fit an SM), which moves what it selected.  Else CTAs of 1024 threads, a
 // cluster of them per unit while that fills no more than the SMs and leaves each CTA 3000 slots (or where a CTA cannot hold them), and the
 // moves over the whole grid.  Measured, us: 512 units of about 1030 / up to 2047 slots moved by their CTAs 14.7 / 48.2, over the grid 16.2 / 51.9
 // (of 2047 each to 1024 68.8 and 67.9); 16 units of up to 4093 slots without a cluster 12.6, with two CTAs 13.3; 4 units of 30000 slots with
 // eight CTAs 19.1, four 24.0, two 29.4.
 cudaError_t launch_evict(PagedEvictArgs& a, int units, int cap, int n_sm, cudaStream_t stream) {
-  const bool small = units > n_sm && cap <= 8192;
+  const bool small = units > n_sm && cap <= 4096;
   a.cluster = 1;
-  while (!small && a.cluster < PE_CLUSTER && (cap > PE_SLOTS * a.cluster || (2 * a.cluster * units <= n_sm && cap / (2 * a.cluster) >= 3000))) a.cluster *= 2;
+  while (!small && a.cluster < PE_CLUSTER && (cap > PE_KEYS * a.cluster || (2 * a.cluster * units <= n_sm && cap / (2 * a.cluster) >= 3000))) a.cluster *= 2;
   a.slots = ((cap + 31) / 32 + a.cluster - 1) / a.cluster * 32;
   a.in_smem = a.slots <= PE_KEYS ? 1 : 0;
   const size_t smem = (size_t)pe_words(a.slots, a.in_smem) * 4;
   void (*kern)(PagedEvictArgs) = small ? k_paged_select<256, true> : k_paged_select<1024, false>;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024);      // (see launch_attention)
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024);      // (see launch_attention)
   if (e == cudaSuccess) e = launch_k(1, kern, dim3(units * a.cluster), dim3(small ? 256 : 1024), smem, stream, a.cluster, a);
   if (e != cudaSuccess || small || a.max_moves == 0) return e;
   // as many blocks as are resident at once (four an SM): their warps take pairs in turn

@@ -140,13 +140,13 @@ __global__ void __launch_bounds__(PP_THREADS) k_paged_append(const PagedAppendAr
 // Selection, a cluster of CTAs per (sequence, KV head): the budget smallest of the keys (falling weight, position), by radix selection; then
 // the kept slots as a bitmap, whose counts give every slot that moves its partner: the i-th kept slot behind the budget goes to the i-th
 // freed slot ahead of it.  Sources and targets are disjoint, so k_paged_move needs no order between its blocks.
-// Each CTA of the cluster has a run of the slots, their keys in shared memory (read from global memory once); a digit's counts
-// are added over distributed shared memory.  Bound by the chain of passes: a digit costs a read of the keys from shared memory and four barriers.
+// Each CTA of the cluster has a run of the slots, their weights, positions and keys in shared memory (read from global memory once); a digit's
+// counts are added over distributed shared memory.  Bound by the chain of passes: a digit costs 1.3 us (a read of the keys from shared memory
+// and four barriers; with a cluster 2.5).
 constexpr int PE_MAX_CAP = 1 << 20;     // slots of a sequence: a bitmap of 128 KB
 constexpr int PE_BITS = 11, PE_BINS = 1 << PE_BITS;      // a digit
 constexpr int PE_CLUSTER = 8;           // CTAs of a unit at most
-constexpr int PE_SLOTS = 128 * 1024;    // slots of a CTA at most (its bitmap and what goes with it: 48 KB)
-constexpr int PE_KEYS = 40 * 1024;      // slots of a CTA whose keys fit shared memory; beyond that a pass reads them again
+constexpr int PE_KEYS = 13 * 1024;      // slots of a CTA whose weights, positions and keys fit shared memory; beyond that a pass reads them again
 constexpr int PM_WARPS = 8;
 constexpr int PM_PAIRS = 4;             // pairs of a warp that are under way at once
 
@@ -160,7 +160,7 @@ struct PagedEvictArgs {
   int* lens_out;
   int* moves;                  // [batch * hkv][1 + 2 max_moves]: count, sources, targets
   int head_bytes, esz;
-  int cluster, slots, in_smem; // CTAs of a unit, most slots of one (a multiple of 32), their keys are kept in shared memory
+  int cluster, slots, in_smem; // CTAs of a unit, most slots of one (a multiple of 32), weights, positions and keys are kept in shared memory
 };
 
 // Order of the weights, heaviest first: 0 = protected, then falling weight (-0 as 0), NaN last.
@@ -223,8 +223,8 @@ __device__ __forceinline__ uint4 ld_cluster_u4(uint32_t addr) {
   return v;
 }
 
-// Shared memory of a selection, in words: counts, bitmap, holes and movers ahead of each of its words, keys.
-__host__ __device__ inline int pe_words(int slots, int in_smem) { return 2 * PE_BINS + slots / 32 * 3 + 4 + (in_smem ? slots : 0); }
+// Shared memory of a selection, in words: counts, weights, positions and keys, bitmap, holes and movers ahead of each of its words.
+__host__ __device__ inline int pe_words(int slots, int in_smem) { return 2 * PE_BINS + slots / 32 * 3 + 4 + (in_smem ? 3 * slots : 0); }
 
 // What moves of a unit, the pairs (source[i], target[i]): weight, position and rows, by n_warps warps, this one the w-th.  A warp takes PM_PAIRS
 // pairs at a time; the K row in the first half of the lanes, the V row in the second (rows of 512 bytes in two turns).  A turn's rows are under
@@ -294,13 +294,17 @@ __device__ __forceinline__ void pe_move(const PagedEvictArgs& a, int unit, const
 template <int THREADS, bool MOVE>
 __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a) {
   extern __shared__ __align__(16) unsigned pe_smem[];
-  unsigned* keys = pe_smem + 2 * PE_BINS;          // behind two sets of counts: [slots], if they are kept here
-  unsigned* bits = keys + (a.in_smem ? a.slots : 0);      // [slots / 32] kept slots of this CTA
+  // behind two sets of counts: weights, positions and keys [slots], if they are kept here; kept slots of this CTA [slots / 32]
+  float* own_weights = reinterpret_cast<float*>(pe_smem + 2 * PE_BINS);
+  int* own_pos = reinterpret_cast<int*>(own_weights + a.slots);
+  unsigned* own_keys = reinterpret_cast<unsigned*>(own_pos + a.slots);
+  unsigned* bits = pe_smem + 2 * PE_BINS + (a.in_smem ? 3 * a.slots : 0);
   int* holes_at = reinterpret_cast<int*>(bits + a.slots / 32);
   int* movers_at = holes_at + a.slots / 32;
   __shared__ int2 warp_sums[32];
   __shared__ __align__(16) int found[4], shared_counts[4];
-  __shared__ unsigned warp_or[32];
+  __shared__ unsigned warp_or[32], the_value;
+  __shared__ uint2 bits_of[2][32];
   __shared__ int groups_of[2][PE_BINS / 64];
   int turn = 0;
   const int CL = MOVE ? 1 : a.cluster, rank = CL > 1 ? (int)cluster_ctarank() : 0, tid = threadIdx.x, lane = tid & 31;
@@ -326,30 +330,48 @@ __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a
   const int* pos = a.pos ? a.pos + base + s0 : nullptr;
   float* weights_out = a.weights_out + base + s0;
   int* pos_out = a.pos_out ? a.pos_out + base + s0 : nullptr;
-  auto pos_of = [&](int j) { return pos ? pos[j] : s0 + j; };
   if (n <= a.budget) {
     if (!MOVE && rank == 0 && tid == 0) moves[0] = 0;
     for (int j = tid; j < ns; j += THREADS) {
       weights_out[j] = weights[j];
-      if (pos_out) pos_out[j] = pos_of(j);
+      if (pos_out) pos_out[j] = pos ? pos[j] : s0 + j;
     }
     return;
   }
   const int seen = a.seen ? a.seen[b] : n;
   auto key_of = [&](int p, float w) { return (p < a.n_sink || p >= seen - a.n_recent) ? 0u : pe_key(w); };
   unsigned any = 0;                                // bits that some position has
-  if (a.in_smem)
-#pragma unroll 8
-    for (int j = tid; j < ns; j += THREADS) {
-      const int p = pos_of(j);
-      keys[j] = key_of(p, weights[j]);
+  if (a.in_smem) {
+    // four slots a load where a KV head's array begins on 16 bytes (behind the last slot there may be anything up to the next multiple of four)
+    const bool by4 = (cap & 3) == 0 && (((uintptr_t)weights | (uintptr_t)pos) & 15) == 0;
+    const int ahead4 = by4 ? ns / 4 : 0;
+#pragma unroll 2
+    for (int i = tid; i < ahead4; i += THREADS) {
+      const float4 w = reinterpret_cast<const float4*>(weights)[i];
+      const int j = s0 + 4 * i;
+      const int4 p = pos ? reinterpret_cast<const int4*>(pos)[i] : make_int4(j, j + 1, j + 2, j + 3);
+      reinterpret_cast<float4*>(own_weights)[i] = w;
+      reinterpret_cast<int4*>(own_pos)[i] = p;
+      reinterpret_cast<uint4*>(own_keys)[i] = make_uint4(key_of(p.x, w.x), key_of(p.y, w.y), key_of(p.z, w.z), key_of(p.w, w.w));
+      any |= (unsigned)(p.x | p.y | p.z | p.w);
+    }
+#pragma unroll 4
+    for (int j = 4 * ahead4 + tid; j < ns; j += THREADS) {
+      const int p = pos ? pos[j] : s0 + j;
+      const float w = weights[j];
+      own_weights[j] = w;
+      own_pos[j] = p;
+      own_keys[j] = key_of(p, w);
       any |= (unsigned)p;
     }
-  else
-    for (int j = tid; j < ns; j += THREADS) any |= (unsigned)pos_of(j);
+  } else {
+    for (int j = tid; j < ns; j += THREADS) any |= (unsigned)(pos ? pos[j] : s0 + j);
+  }
+  auto pos_of = [&](int j) { return a.in_smem ? own_pos[j] : pos ? pos[j] : s0 + j; };
+  auto weight_of = [&](int j) { return a.in_smem ? own_weights[j] : weights[j]; };
+  auto key = [&](int j) { return a.in_smem ? own_keys[j] : key_of(pos_of(j), weight_of(j)); };
   any = __reduce_or_sync(0xffffffffu, any);
   if (lane == 0) warp_or[tid >> 5] = any;
-  auto key = [&](int j) { return a.in_smem ? keys[j] : key_of(pos_of(j), weights[j]); };
   // The need-th smallest value of at most `width` bits that `get` gives for the slots it says true of: the value, how many are below it, how many
   // equal it.  (Where all values of a prefix are wanted, the rest of the digits are: value = the largest with that prefix.)
   auto select = [&](auto get, int width, int need, unsigned& value, int& below, int& equal) {
@@ -364,10 +386,23 @@ __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a
 #pragma unroll
       for (int i = tid; i < PE_BINS / 4; i += THREADS) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
       __syncthreads();
+      // Between the first and the last digit: bits that all / some of the values counted here have.  Where one value is all there is (slots that
+      // nobody attends to weigh 0) no further digit is needed.
+      const bool look = CL == 1 && shift > 0 && shift + PE_BITS < width;
+      unsigned all_of = 0xffffffffu, some_of = 0;
 #pragma unroll 4
       for (int j = tid; j < ns; j += THREADS) {
         unsigned k;
-        if (get(j, k) && (k & mask) == prefix) atomicAdd(&hist[(k >> shift) & digit], 1u);
+        if (get(j, k) && (k & mask) == prefix) {
+          atomicAdd(&hist[(k >> shift) & digit], 1u);
+          all_of &= k;
+          some_of |= k;
+        }
+      }
+      if (look) {
+        all_of = __reduce_and_sync(0xffffffffu, all_of);
+        some_of = __reduce_or_sync(0xffffffffu, some_of);
+        if (lane == 0) bits_of[turn][tid >> 5] = make_uint2(all_of, some_of);
       }
       __syncthreads();
       // counts of 64 bins each, a warp a group; the first warp finds the group in which the need-th lies, then the bin
@@ -412,8 +447,24 @@ __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a
           found[1] = second ? before + h.x : before;
           found[2] = second ? h.y : h.x;
         }
+        if (look) {
+          const uint2 x = lane < THREADS / 32 ? bits_of[turn][lane] : make_uint2(0xffffffffu, 0u);
+          all_of = __reduce_and_sync(0xffffffffu, x.x);
+          some_of = __reduce_or_sync(0xffffffffu, x.y);
+          if (lane == 0) {
+            found[3] = all_of == some_of;
+            the_value = all_of;
+          }
+        }
       }
       __syncthreads();
+      if (look && found[3]) {
+        prefix = the_value;
+        mask = 0xffffffffu;
+        below += found[1];
+        equal = found[2];
+        break;
+      }
       prefix |= (unsigned)found[0] << shift;
       mask |= digit << shift;
       below += found[1];
@@ -511,7 +562,7 @@ __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a
     for (int i = 0; i < AT_ONCE; ++i) {
       const int w = w4 + i * (THREADS / 32);
       const bool stays = w < words && ((bits[w] & ahead(w)) >> lane & 1);
-      weight[i] = stays ? weights[w * 32 + lane] : 0.f;
+      weight[i] = stays ? weight_of(w * 32 + lane) : 0.f;
       p[i] = stays && pos_out ? pos_of(w * 32 + lane) : 0;
     }
 #pragma unroll
