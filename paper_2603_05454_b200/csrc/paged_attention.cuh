@@ -827,17 +827,12 @@ __global__ void __launch_bounds__(PW_THREADS) k_paged_weights(const PagedAttnArg
   }
   const long long base = ((long long)b * a.pv.hkv + kvh) * cap;
   const int j = j0 + threadIdx.x;
-  float sum[KPT];
-#pragma unroll
-  for (int k = 0; k < KPT; ++k) sum[k] = j + k * PW_THREADS < len && a.weights_in ? a.weights_in[base + j + k * PW_THREADS] : 0.f;
-  __syncthreads();
   // scores of row x of the group's: `heads` of a row lie one behind the other, the next row's a.hq heads on
   const float* src = a.scores + ((long long)rs.first * a.hq + kvh * a.group) * cap + j;
   const long long wrap = (long long)(a.hq - a.group + 1) * cap;
   int h = 0;
-  float add[KPT] = {};
-  for (int x = 0; x < n; x += ROWS) {
-    float s[ROWS][KPT];
+  float s[ROWS][KPT];
+  auto load = [&](int x) {
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
 #pragma unroll
@@ -846,10 +841,19 @@ __global__ void __launch_bounds__(PW_THREADS) k_paged_weights(const PagedAttnArg
       src += last ? wrap : cap;
       h = last ? 0 : h;
     }
+  };
+  load(0);                                        // (while the rows' sums are on their way)
+  float sum[KPT];
+#pragma unroll
+  for (int k = 0; k < KPT; ++k) sum[k] = j + k * PW_THREADS < len && a.weights_in ? a.weights_in[base + j + k * PW_THREADS] : 0.f;
+  __syncthreads();
+  float add[KPT] = {};
+  for (int x = 0; x < n; x += ROWS) {
 #pragma unroll
     for (int i = 0; i < ROWS; ++i)
 #pragma unroll
       for (int k = 0; k < KPT; ++k) add[k] += pa_exp2(s[i][k] - lse2[min(x + i, n - 1)]);
+    if (x + ROWS < n) load(x + ROWS);
   }
 #pragma unroll
   for (int k = 0; k < KPT; ++k)
