@@ -539,8 +539,9 @@ __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a
         holes += (int)x[r].x;
         movers += (int)x[r].y;
       }
-    // Nobody leaves while another reads its counts; that orders no memory, and an arrival with release would wait for the stores below.
-    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    // Nobody leaves while another reads its counts: arrived here, behind those reads and ahead of the stores below (an arrival behind them would
+    // wait for them).
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   }
   for (int w = w0; w < w1; ++w) {
     holes_at[w] = at.x;
@@ -582,7 +583,7 @@ __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a
       }
     }
   }
-  if (CL > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+  if (CL > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   if (MOVE) {
     __syncthreads();
     pe_move(a, unit, src, dst, n_moves, tid >> 5, THREADS / 32);
