@@ -130,18 +130,19 @@ cudaError_t launch_attention(const PagedAttnArgs& a0, int tiles, cudaStream_t st
   if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kCta);
   if (e != cudaSuccess) return e;
   const long long cap = (long long)a.pv.max_pages * a.pv.page;
-  const long long most = ((cap + PA_CHUNK - 1) / PA_CHUNK + PA_UNIT_COST) * a.pv.batch * a.pv.hkv * tiles;       // numbers to deal, if every sequence were full
-  // At most 32 CTAs a unit: one of them adds the parts.  One sequence of 8000 / 30011 slots of 4 KV heads: 16.0 / 27.4 us, without the bound (74
+  a.lanes = std::min(tiles, PA_LANES);
+  const long long units = (long long)a.pv.batch * a.pv.hkv * ((tiles + a.lanes - 1) / a.lanes);      // of a lane
+  const long long most = ((cap + PA_CHUNK - 1) / PA_CHUNK + PA_UNIT_COST) * units;       // numbers to deal, if every sequence were full
+  // At most 32 runs a unit: one CTA adds the parts.  One sequence of 8000 / 30011 slots of 4 KV heads: 16.0 / 27.4 us, without the bound (74
   // parts) 21.5 / 30.3, with 16 16.8 / 36.3.
-  const long long parts = 32ll * a.pv.batch * a.pv.hkv * tiles;
-  a.n_cta = (int)std::min({most, parts, (long long)std::min(n_per_sm * n_sm, pa_max_ctas(DH))});
-  e = launch_k(1, kern, dim3(a.n_cta), dim3(PA_THREADS), (size_t)smem, stream, a);
+  a.n_runs = (int)std::min({most, 32 * units, (long long)std::min(n_per_sm * n_sm, pa_max_ctas(DH)) / a.lanes});
+  e = launch_k(1, kern, dim3(a.n_runs * a.lanes), dim3(PA_THREADS), (size_t)smem, stream, a);
   if (e != cudaSuccess || !a.scores) return e;
   // a slot a thread, and four where that still leaves four blocks an SM
-  const long long units = (long long)a.pv.batch * a.pv.hkv;
-  const int kpt = units * ((cap + 4 * PW_THREADS - 1) / (4 * PW_THREADS)) >= 4 * n_sm ? 4 : 1;
+  const long long heads = (long long)a.pv.batch * a.pv.hkv;
+  const int kpt = heads * ((cap + 4 * PW_THREADS - 1) / (4 * PW_THREADS)) >= 4 * n_sm ? 4 : 1;
   const int key_blocks = (int)((cap + kpt * PW_THREADS - 1) / (kpt * PW_THREADS));
-  return launch_k(1, kpt == 4 ? k_paged_weights<4> : k_paged_weights<1>, dim3((unsigned)(units * key_blocks)), dim3(PW_THREADS), (size_t)a.max_rows * a.group * 4,
+  return launch_k(1, kpt == 4 ? k_paged_weights<4> : k_paged_weights<1>, dim3((unsigned)(heads * key_blocks)), dim3(PW_THREADS), (size_t)a.max_rows * a.group * 4,
                   stream, a, key_blocks);
 }
 
@@ -262,7 +263,7 @@ int lsp_paged_attention(const lsp_paged_kv* kv, const void* q, long long ldq, in
   a.hq = n_heads;
   a.max_rows = max_rows;
   a.n_rows = n_rows;
-  a.n_cta = 0;
+  a.n_runs = 0;
   a.scale_log2 = scale * 1.4426950408889634f;
   a.lse = lse;
   a.part_o = (float*)(ws + L.part_o);

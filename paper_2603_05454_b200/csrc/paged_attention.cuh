@@ -10,6 +10,8 @@
 //    numbered through, with room for what a unit costs besides, and each CTA of a grid that fills the SMs takes an equal run of the
 //    numbers, whatever the lengths are.  A unit that one CTA holds whole is written by it; the parts (m, l, o) of a unit that a run's
 //    end cuts go to the workspace, and the last of its CTAs to arrive adds them in their order: the same bits every time.
+//  * Where there are several tiles of rows, as many CTAs share a run, a tile ("lane") each: they go over the same slots at the same time, so
+//    that all but one of them find the rows in L2.
 //  * A warp takes 16 slots of a chunk and loads them itself: a ring of its own in shared memory, filled by cp.async, page ids a window
 //    of chunks ahead of the rows they lead to, the queries of the next unit with its first chunk.  The warps of a CTA meet only where a
 //    unit begins and ends.
@@ -17,8 +19,6 @@
 //    issue is what competes with the bytes: 16 slots cost it some 300 instructions (655 once, when 16 x 2047 slots took 77 us).
 // Measured on one B200 (copy rate 6.53 TB/s): 16 x 12000 slots of 32 KV heads of 128 352 us = 6.75 TB/s; 16 x 2047 ragged (406 MB) 69.7 us =
 // 5.8 TB/s, of which 60 are the stream, 4.5 the chain lengths -> pages -> rows, 5 the uneven end and the adding of parts.
-// A second tile of rows reads the cache again (28 pairs over 32 x 30000 slots 420 us, 7 pairs 223): two tiles that share what is read in a
-// CTA of eight warps took 369, and 24 pairs of heads of 64 and short caches longer than so; not kept.
 #pragma once
 #include "attention_mma.cuh"
 #include "paged_common.cuh"
@@ -30,6 +30,10 @@ constexpr int PA_WARPS = 4;
 constexpr int PA_THREADS = PA_WARPS * 32;
 constexpr int PA_ROWS = 16;             // (row, head) pairs of a unit
 constexpr int PA_MAX_BATCH = 1024;
+// CTAs that share a run at most.  28 / 56 pairs over 32 x 30000 slots of 4 heads: 305 / 591 us with two, 421 / 822 each for itself (the warps'
+// instructions, not the bytes, are the time then); with four the same, and blocks of one to eight rows a sequence 589 where two take 453 to
+// 489 and each for itself 528.
+constexpr int PA_LANES = 2;
 // CTAs of a launch at most (workspaces are sized by it), and on an SM: those that 64 warps' registers allow, so that 128 KB are in flight
 __host__ __device__ constexpr int pa_max_ctas(int dh) { return dh == 64 ? 1024 : 512; }
 __host__ __device__ constexpr int pa_ctas_sm(int dh, int esz) { return dh == 64 && esz == 2 ? 4 : dh == 128 && esz == 4 ? 1 : 2; }
@@ -43,12 +47,13 @@ struct PagedAttnArgs {
   void* out;
   long long ldq, ldo;
   const int *lens, *row_off;
-  int hq, group, max_rows, n_rows, n_cta;
+  int hq, group, max_rows, n_rows;
+  int n_runs, lanes;           // CTA x has run x / lanes; of each group of `lanes` tiles of rows the (x % lanes)-th
   float scale_log2;
   float* lse;                  // [n_rows][hq] or null
-  unsigned* arrived;           // [n_cta]: parts of the cut unit that begins in CTA i's run; 0 between calls
-  float* part_o;               // [2 n_cta][16][dh]
-  float2* part_ml;             // [2 n_cta][16]: m (in log2 units), l
+  unsigned* arrived;           // [CTA]: parts of the cut unit that begins in the CTA's run; 0 between calls
+  float* part_o;               // [2 CTAs][16][dh]
+  float2* part_ml;             // [2 CTAs][16]: m (in log2 units), l
   float* scores;               // [n_rows][hq][capacity] in log2 units, or null: no weights wanted
   float* row_lse;              // [n_rows][hq]: log2 of the sum of exponentials (with weights)
   const float* weights_in;
@@ -94,7 +99,7 @@ __device__ __forceinline__ void pa_prefix(const PagedAttnArgs& a, int* pre) {
       if (b < B) {
         const RowSpan rs = pg_rows(a.pv, a.row_off, b, a.max_rows, a.n_rows);
         const int chunks = pa_chunks(pg_len(a.pv, B > 32 ? pre[b] : a.lens[b]));
-        n = chunks == 0 ? 0 : (chunks + PA_UNIT_COST) * a.pv.hkv * ((rs.n * a.group + PA_ROWS - 1) / PA_ROWS);
+        n = chunks == 0 ? 0 : (chunks + PA_UNIT_COST) * a.pv.hkv * pg_div(rs.n * a.group + PA_ROWS * a.lanes - 1, PA_ROWS * a.lanes);
       }
       int x = n;
 #pragma unroll
@@ -120,17 +125,17 @@ __device__ __forceinline__ void pa_prefetch(const PagedAttnArgs& a) {
   pg_prefetch_table(a.pv);
 }
 
-// How the numbers are dealt: CTA i of n (those that get at least one) has numbers [run(i), run(i + 1)), run(i) = floor(total i / n).
+// How the numbers are dealt: run i of n (those that get at least one) is numbers [run(i), run(i + 1)), run(i) = floor(total i / n).
 struct PaDeal {
   int total, n, q, r;
-  __device__ __forceinline__ PaDeal(int total_, int n_cta) : total(total_), n(min(total_, n_cta)), q(0), r(0) {
+  __device__ __forceinline__ PaDeal(int total_, int n_runs) : total(total_), n(min(total_, n_runs)), q(0), r(0) {
     if (n > 0) {
       q = total / n;
       r = total - q * n;
     }
   }
   __device__ __forceinline__ int run(int i) const { return i * q + pg_div(i * r, n); }
-  // the CTA whose run holds number c (the estimate is off by one at most: 2^-24 of at most 1024, and the runs' rounding)
+  // the run that holds number c (the estimate is off by one at most: 2^-24 of at most 1024, and the runs' rounding)
   __device__ __forceinline__ int owner(int c) const {
     int i = min(n - 1, (int)((float)c / (float)total * (float)n));
     while (run(i) > c) --i;
@@ -145,10 +150,12 @@ struct PaPlace {
   int u0, left;                 // the number of the unit's first chunk; chunks of the unit that belong to the run, from here on
   __device__ __forceinline__ int next() const { return u0 + chunks + PA_UNIT_COST; }      // the following unit
 };
-// The place of the first chunk at or behind number c (some numbers are no chunks); left = 0 where the run holds none.
+// The place of the first chunk at or behind number c (some numbers are no chunks, and where a sequence's last group of tiles is not full its units
+// are not those of all lanes); left = 0 where the run holds none.
 __device__ __forceinline__ PaPlace pa_place(const PagedAttnArgs& a, const int* pre, int c, int hi) {
   PaPlace p;
   p.left = 0;
+  const int lane = a.lanes == 1 ? 0 : (int)blockIdx.x % a.lanes;
   while (c < hi) {
     int lo = 0, up = a.pv.batch;                   // pre[lo] <= c < pre[up]
     while (up - lo > 1) {
@@ -159,14 +166,14 @@ __device__ __forceinline__ PaPlace pa_place(const PagedAttnArgs& a, const int* p
     const int n = a.lens[lo], cap = pg_capacity(a.pv);
     p.len = n > cap ? cap : n;
     p.chunks = pa_chunks(p.len);
-    // (quotients: a sequence's KV heads times tiles, at most 2^20 by the call's limits)
-    const int span = p.chunks + PA_UNIT_COST, tiles = pg_div(pre[lo + 1] - pre[lo], span * a.pv.hkv);
+    // (quotients: a sequence's KV heads times groups of tiles, at most 2^20 by the call's limits)
+    const int span = p.chunks + PA_UNIT_COST, groups = pg_div(pre[lo + 1] - pre[lo], span * a.pv.hkv);
     const int u = pg_div(c - pre[lo], span);
     p.u0 = pre[lo] + u * span;
     p.chunk = c - p.u0;
-    p.kvh = pg_div(u, tiles);
-    p.rt = u - p.kvh * tiles;
-    if (p.chunk < p.chunks) {
+    p.kvh = pg_div(u, groups);
+    p.rt = (u - p.kvh * groups) * a.lanes + lane;
+    if (p.chunk < p.chunks && (a.lanes == 1 || p.rt * PA_ROWS < pg_rows(a.pv, a.row_off, lo, a.max_rows, a.n_rows).n * a.group)) {
       p.left = min(p.chunks - p.chunk, hi - c);
       break;
     }
@@ -175,8 +182,8 @@ __device__ __forceinline__ PaPlace pa_place(const PagedAttnArgs& a, const int* p
   return p;
 }
 
-// A part of a cut unit, noted until the run's end: the unit, and CTAs first .. last, which have a part each; the first one's is its second
-// part where the unit begins in its run.
+// A part of a cut unit, noted until the run's end: the unit, and runs first .. last, whose CTAs (of this lane) have a part each; the first one's
+// is its second part where the unit begins in its run.
 struct PaCut {
   PaPlace p;
   int first, last, second;
@@ -452,14 +459,16 @@ __device__ __forceinline__ void pa_join(const PagedAttnArgs& a, const PaCut* cut
     bool last = false;
     if (c.p.left > 0) {
       __threadfence();
-      last = atomicAdd(a.arrived + c.first, 1u) == (unsigned)(c.last - c.first);
-      if (last) a.arrived[c.first] = 0;
+      unsigned* arrived = a.arrived + c.first * a.lanes + blockIdx.x % a.lanes;
+      last = atomicAdd(arrived, 1u) == (unsigned)(c.last - c.first);
+      if (last) *arrived = 0;
       __threadfence();
     }
     mine[threadIdx.x] = last;
   }
   __syncthreads();
   // the rows of both units dealt to the warps
+  const int lane_of = blockIdx.x % a.lanes;
   int skip = w;
 #pragma unroll 1
   for (int which = 0; which < 2; ++which) {
@@ -477,7 +486,7 @@ __device__ __forceinline__ void pa_join(const PagedAttnArgs& a, const PaCut* cut
 #pragma unroll 1
       for (int k0 = 0; k0 < n; k0 += 32) {
         const int k = min(k0 + lane, n - 1);
-        const int slot = (2 * (i0 + k) + (k == 0 ? second : 0)) * PA_ROWS + r;
+        const int slot = (2 * ((i0 + k) * a.lanes + lane_of) + (k == 0 ? second : 0)) * PA_ROWS + r;
         const float2 x = __ldcg(a.part_ml + slot);
         float y[PA_AHEAD][VEC], f = 0.f;
 #pragma unroll 1
@@ -545,9 +554,10 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 2)) k_paged_attn_mm
   pdl_wait();
   pa_prefix(a, pre);
   pa_empty<bf16, DH>(a, pre);
-  const PaDeal deal(pre[a.pv.batch], a.n_cta);
-  if ((int)blockIdx.x >= deal.n) return;
-  const int lo = deal.run(blockIdx.x), hi = deal.run(blockIdx.x + 1);
+  const PaDeal deal(pre[a.pv.batch], a.n_runs);
+  const int run = (int)blockIdx.x / a.lanes;
+  if (run >= deal.n) return;
+  const int lo = deal.run(run), hi = deal.run(run + 1);
   PaPlace p = pa_place(a, pre, lo, hi);
   if (p.left == 0) return;
   __shared__ PaCut cut[2];
@@ -703,9 +713,10 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 4)) k_paged_attn_si
   pdl_wait();
   pa_prefix(a, pre);
   pa_empty<float, DH>(a, pre);
-  const PaDeal deal(pre[a.pv.batch], a.n_cta);
-  if ((int)blockIdx.x >= deal.n) return;
-  const int lo = deal.run(blockIdx.x), hi = deal.run(blockIdx.x + 1);
+  const PaDeal deal(pre[a.pv.batch], a.n_runs);
+  const int run = (int)blockIdx.x / a.lanes;
+  if (run >= deal.n) return;
+  const int lo = deal.run(run), hi = deal.run(run + 1);
   PaPlace p = pa_place(a, pre, lo, hi);
   if (p.left == 0) return;
   __shared__ PaCut cut[2];
