@@ -308,7 +308,7 @@ int lsp_paged_append(const lsp_paged_kv* kv, const void* k_new, const void* v_ne
  * A row over no slot (lens[b] = 0), or whose scores are all -inf, gets 0 and lse -inf.  q, out: packed rows as for the append, ldq and ldo
  * elements apart.  The slots are split over the device and the parts joined in a fixed order: the same inputs give the same bits.
  * Accumulation in fp32; bf16 softmax weights enter the product with V as a sum of two.  Meant for up to some dozens of (row, head)
- * pairs per KV head; a tile of 16 of them reads the cache once.
+ * pairs per KV head: every 32 of them read the cache once.
  * workspace: device, 256-byte aligned, lsp_paged_attention_workspace() bytes (for weights it holds the scores).  Its first 4096 bytes hold
  * counters: the caller clears them once, every call leaves them clear; the rest may hold anything.  Calls that share a workspace must not overlap
  * on the device. */

@@ -130,13 +130,13 @@ cudaError_t launch_attention(const PagedAttnArgs& a0, int tiles, cudaStream_t st
   if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kCta);
   if (e != cudaSuccess) return e;
   const long long cap = (long long)a.pv.max_pages * a.pv.page;
-  a.lanes = std::min(tiles, PA_LANES);
-  const long long units = (long long)a.pv.batch * a.pv.hkv * ((tiles + a.lanes - 1) / a.lanes);      // of a lane
+  a.lane_bits = tiles > 1 ? PA_LANE_BITS : 0;
+  const long long units = (long long)a.pv.batch * a.pv.hkv * ((tiles + (1 << a.lane_bits) - 1) >> a.lane_bits);      // of a lane
   const long long most = ((cap + PA_CHUNK - 1) / PA_CHUNK + PA_UNIT_COST) * units;       // numbers to deal, if every sequence were full
   // At most 32 runs a unit: one CTA adds the parts.  One sequence of 8000 / 30011 slots of 4 KV heads: 16.0 / 27.4 us, without the bound (74
   // parts) 21.5 / 30.3, with 16 16.8 / 36.3.
-  a.n_runs = (int)std::min({most, 32 * units, (long long)std::min(n_per_sm * n_sm, pa_max_ctas(DH)) / a.lanes});
-  e = launch_k(1, kern, dim3(a.n_runs * a.lanes), dim3(PA_THREADS), (size_t)smem, stream, a);
+  a.n_runs = (int)std::min({most, 32 * units, (long long)std::min(n_per_sm * n_sm, pa_max_ctas(DH)) >> a.lane_bits});
+  e = launch_k(1, kern, dim3(a.n_runs << a.lane_bits), dim3(PA_THREADS), (size_t)smem, stream, a);
   if (e != cudaSuccess || !a.scores) return e;
   // a slot a thread, and four where that still leaves four blocks an SM
   const long long heads = (long long)a.pv.batch * a.pv.hkv;

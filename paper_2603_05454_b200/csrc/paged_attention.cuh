@@ -33,7 +33,7 @@ constexpr int PA_MAX_BATCH = 1024;
 // CTAs that share a run at most.  28 / 56 pairs over 32 x 30000 slots of 4 heads: 305 / 591 us with two, 421 / 822 each for itself (the warps'
 // instructions, not the bytes, are the time then); with four the same, and blocks of one to eight rows a sequence 589 where two take 453 to
 // 489 and each for itself 528.
-constexpr int PA_LANES = 2;
+constexpr int PA_LANE_BITS = 1;
 // CTAs of a launch at most (workspaces are sized by it), and on an SM: those that 64 warps' registers allow, so that 128 KB are in flight
 __host__ __device__ constexpr int pa_max_ctas(int dh) { return dh == 64 ? 1024 : 512; }
 __host__ __device__ constexpr int pa_ctas_sm(int dh, int esz) { return dh == 64 && esz == 2 ? 4 : dh == 128 && esz == 4 ? 1 : 2; }
@@ -48,7 +48,9 @@ struct PagedAttnArgs {
   long long ldq, ldo;
   const int *lens, *row_off;
   int hq, group, max_rows, n_rows;
-  int n_runs, lanes;           // CTA x has run x / lanes; of each group of `lanes` tiles of rows the (x % lanes)-th
+  int n_runs, lane_bits;       // CTA x has run x >> lane_bits; of each group of 1 << lane_bits tiles of rows the one of its lower bits
+  __device__ __forceinline__ int lanes() const { return 1 << lane_bits; }
+  __device__ __forceinline__ int lane() const { return blockIdx.x & ((1 << lane_bits) - 1); }
   float scale_log2;
   float* lse;                  // [n_rows][hq] or null
   unsigned* arrived;           // [CTA]: parts of the cut unit that begins in the CTA's run; 0 between calls
@@ -99,7 +101,7 @@ __device__ __forceinline__ void pa_prefix(const PagedAttnArgs& a, int* pre) {
       if (b < B) {
         const RowSpan rs = pg_rows(a.pv, a.row_off, b, a.max_rows, a.n_rows);
         const int chunks = pa_chunks(pg_len(a.pv, B > 32 ? pre[b] : a.lens[b]));
-        n = chunks == 0 ? 0 : (chunks + PA_UNIT_COST) * a.pv.hkv * pg_div(rs.n * a.group + PA_ROWS * a.lanes - 1, PA_ROWS * a.lanes);
+        n = chunks == 0 ? 0 : (chunks + PA_UNIT_COST) * a.pv.hkv * ((rs.n * a.group + PA_ROWS * a.lanes() - 1) / PA_ROWS >> a.lane_bits);
       }
       int x = n;
 #pragma unroll
@@ -155,7 +157,6 @@ struct PaPlace {
 __device__ __forceinline__ PaPlace pa_place(const PagedAttnArgs& a, const int* pre, int c, int hi) {
   PaPlace p;
   p.left = 0;
-  const int lane = a.lanes == 1 ? 0 : (int)blockIdx.x % a.lanes;
   while (c < hi) {
     int lo = 0, up = a.pv.batch;                   // pre[lo] <= c < pre[up]
     while (up - lo > 1) {
@@ -172,8 +173,8 @@ __device__ __forceinline__ PaPlace pa_place(const PagedAttnArgs& a, const int* p
     p.u0 = pre[lo] + u * span;
     p.chunk = c - p.u0;
     p.kvh = pg_div(u, groups);
-    p.rt = (u - p.kvh * groups) * a.lanes + lane;
-    if (p.chunk < p.chunks && (a.lanes == 1 || p.rt * PA_ROWS < pg_rows(a.pv, a.row_off, lo, a.max_rows, a.n_rows).n * a.group)) {
+    p.rt = ((u - p.kvh * groups) << a.lane_bits) + a.lane();
+    if (p.chunk < p.chunks && (a.lane_bits == 0 || p.rt * PA_ROWS < pg_rows(a.pv, a.row_off, lo, a.max_rows, a.n_rows).n * a.group)) {
       p.left = min(p.chunks - p.chunk, hi - c);
       break;
     }
@@ -459,7 +460,7 @@ __device__ __forceinline__ void pa_join(const PagedAttnArgs& a, const PaCut* cut
     bool last = false;
     if (c.p.left > 0) {
       __threadfence();
-      unsigned* arrived = a.arrived + c.first * a.lanes + blockIdx.x % a.lanes;
+      unsigned* arrived = a.arrived + (c.first << a.lane_bits) + a.lane();
       last = atomicAdd(arrived, 1u) == (unsigned)(c.last - c.first);
       if (last) *arrived = 0;
       __threadfence();
@@ -468,7 +469,6 @@ __device__ __forceinline__ void pa_join(const PagedAttnArgs& a, const PaCut* cut
   }
   __syncthreads();
   // the rows of both units dealt to the warps
-  const int lane_of = blockIdx.x % a.lanes;
   int skip = w;
 #pragma unroll 1
   for (int which = 0; which < 2; ++which) {
@@ -486,7 +486,7 @@ __device__ __forceinline__ void pa_join(const PagedAttnArgs& a, const PaCut* cut
 #pragma unroll 1
       for (int k0 = 0; k0 < n; k0 += 32) {
         const int k = min(k0 + lane, n - 1);
-        const int slot = (2 * ((i0 + k) * a.lanes + lane_of) + (k == 0 ? second : 0)) * PA_ROWS + r;
+        const int slot = (2 * (((i0 + k) << a.lane_bits) + a.lane()) + (k == 0 ? second : 0)) * PA_ROWS + r;
         const float2 x = __ldcg(a.part_ml + slot);
         float y[PA_AHEAD][VEC], f = 0.f;
 #pragma unroll 1
@@ -555,7 +555,7 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 2)) k_paged_attn_mm
   pa_prefix(a, pre);
   pa_empty<bf16, DH>(a, pre);
   const PaDeal deal(pre[a.pv.batch], a.n_runs);
-  const int run = (int)blockIdx.x / a.lanes;
+  const int run = (int)blockIdx.x >> a.lane_bits;
   if (run >= deal.n) return;
   const int lo = deal.run(run), hi = deal.run(run + 1);
   PaPlace p = pa_place(a, pre, lo, hi);
@@ -714,7 +714,7 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 4)) k_paged_attn_si
   pa_prefix(a, pre);
   pa_empty<float, DH>(a, pre);
   const PaDeal deal(pre[a.pv.batch], a.n_runs);
-  const int run = (int)blockIdx.x / a.lanes;
+  const int run = (int)blockIdx.x >> a.lane_bits;
   if (run >= deal.n) return;
   const int lo = deal.run(run), hi = deal.run(run + 1);
   PaPlace p = pa_place(a, pre, lo, hi);
