@@ -108,8 +108,11 @@ cudaError_t launch_attention(const PagedAttnArgs& a0, int tiles, cudaStream_t st
     kern = a16 ? k_paged_attn_mma<DH, true> : k_paged_attn_mma<DH, false>;
   } else {
     // (pages of other sizes: every slot's page is looked up, by the one kernel for any number of rows)
-    kern = !a16 ? k_paged_attn_simt<DH, 16, false> : a.q_rows == 1 ? k_paged_attn_simt<DH, 1, true> : a.q_rows == 2 ? k_paged_attn_simt<DH, 2, true>
-         : a.q_rows <= 4 ? k_paged_attn_simt<DH, 4, true> : a.q_rows <= 8 ? k_paged_attn_simt<DH, 8, true> : k_paged_attn_simt<DH, 16, true>;
+    int rows = 1;
+    while (rows < a.q_rows || (!a16 && rows < PA_ROWS)) rows *= 2;
+    a.q_rows = rows;
+    kern = !a16 ? k_paged_attn_simt<DH, 16, false> : rows == 1 ? k_paged_attn_simt<DH, 1, true> : rows == 2 ? k_paged_attn_simt<DH, 2, true>
+         : rows == 4 ? k_paged_attn_simt<DH, 4, true> : rows == 8 ? k_paged_attn_simt<DH, 8, true> : k_paged_attn_simt<DH, 16, true>;
   }
   // As many CTAs an SM as its registers hold, unless their shared memory forbids; as many rows added at a time as there is room for.
   constexpr int kStatic = 128, kSm = 228 * 1024, kCta = 227 * 1024 - kStatic, kOwn = 1024 + kStatic;
@@ -148,8 +151,8 @@ cudaError_t launch_attention(const PagedAttnArgs& a0, int tiles, cudaStream_t st
 
 // Where there are more units than SMs, of at most 4096 slots: a CTA of 256 threads each (four fit an SM), which moves what it selected.  Else CTAs of 1024 threads, a
 // cluster of them per unit while that fills no more than the SMs and leaves each CTA 3000 slots (or where a CTA cannot hold them), and the
-// moves over the whole grid.  Measured, us: 512 units of about 1030 / up to 2047 slots moved by their CTAs 14.7 / 48.2, over the grid 16.2 / 51.9
-// (of 2047 each to 1024 68.8 and 67.9); 16 units of up to 4093 slots without a cluster 12.6, with two CTAs 13.3; 4 units of 30000 slots with
+// moves over the whole grid.  Measured, us: 512 units of about 1030 / up to 2047 slots moved by their CTAs 12.4 / 44.8, over the grid 14.2 / 46.8
+// (of 2047 each to 1024 64.4 and 64.3); 16 units of up to 4093 slots without a cluster 12.6, with two CTAs 13.3; 4 units of 30000 slots with
 // eight CTAs 19.1, four 24.0, two 29.4.
 cudaError_t launch_evict(PagedEvictArgs& a, int units, int cap, int n_sm, cudaStream_t stream) {
   const bool small = units > n_sm && cap <= 4096;

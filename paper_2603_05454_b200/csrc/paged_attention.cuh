@@ -17,8 +17,8 @@
 //    unit begins and ends.
 //  * mma.sync m16n8k16, not tcgen05: a tile has at most 16 rows (often one), an M of 128 would be 1/8 to 1/128 full.  What a warp has to
 //    issue is what competes with the bytes: 16 slots cost it some 300 instructions (655 once, when 16 x 2047 slots took 77 us).
-// Measured on one B200 (copy rate 6.53 TB/s): 16 x 12000 slots of 32 KV heads of 128 352 us = 6.75 TB/s; 16 x 2047 ragged (406 MB) 69.7 us =
-// 5.8 TB/s, of which 60 are the stream, 4.5 the chain lengths -> pages -> rows, 5 the uneven end and the adding of parts.
+// Measured on one B200 (copy rate 6.53 TB/s): 16 x 12000 slots of 32 KV heads of 128 350 us = 6.79 TB/s; 16 x 2047 ragged (406 MB) 67.7 us =
+// 6.0 TB/s, of which 60 are the stream, 4 the chain lengths -> pages -> rows, 4 the uneven end and the adding of parts.
 #pragma once
 #include "attention_mma.cuh"
 #include "paged_common.cuh"
@@ -60,7 +60,7 @@ struct PagedAttnArgs {
   float* row_lse;              // [n_rows][hq]: log2 of the sum of exponentials (with weights)
   const float* weights_in;
   float* weights_out;
-  int q_rows, merge_rows;      // rows of a query tile in shared memory; rows that the warps' parts are added for at a time
+  int q_rows, merge_rows;      // rows of a query tile in shared memory (fp32: the kernel's NR); rows that the warps' parts are added for at a time
 };
 
 // Shared memory: queries (tiles in turn, a unit each), rings, parts of the warps, their (m, l), chunks before each sequence.
@@ -72,9 +72,8 @@ struct PaSmem {
   // Tiles of queries: those of as many units as chunks are asked for ahead, the next one's, and where the queries are not copied to registers at
   // once the present one's (a warp may still be in it when another has reached the next).
   static constexpr int Q_TILES = sizeof(T) == 4 ? STAGES + 1 : STAGES;
-  static constexpr int Q_ROW = DH * (int)sizeof(T) + (sizeof(T) == 4 ? 16 : 0);
   static constexpr int RINGS = PA_WARPS * STAGES * STAGE;
-  __host__ __device__ static int q_tile(int q_rows) { return q_rows * Q_ROW; }
+  __host__ __device__ static int q_tile(int q_rows) { return q_rows * DH * (int)sizeof(T); }
   __host__ __device__ static int rings(int q_rows) { return (Q_TILES * q_tile(q_rows) + 127) / 128 * 128; }
   __host__ __device__ static int merge(int q_rows) { return rings(q_rows) + RINGS; }
   __host__ __device__ static int ml(int q_rows, int merge_rows) { return merge(q_rows) + PA_WARPS * merge_rows * DH * 4; }
@@ -210,11 +209,11 @@ template <typename T, int DH>
 __device__ __forceinline__ int pa_at(int r, int c) {
   return r * DH * (int)sizeof(T) + ((c ^ (r & 7)) << 4);
 }
-// The same in a tile of queries; fp32: not exchanged, the second half of a row 16 bytes on (half-warps read one half each).
+// The same in a tile of queries; fp32: not exchanged (eight lanes read eight chunks of one row).
 template <typename T, int DH>
 __device__ __forceinline__ int pa_q_at(int r, int c) {
   if constexpr (sizeof(T) == 2) return pa_at<T, DH>(r, c);
-  else return r * PaSmem<T, DH>::Q_ROW + c * 16 + (c >= DH / 8 ? 16 : 0);
+  else return r * DH * 4 + c * 16;
 }
 
 // One warp's loads: the rows of its 16 slots of a chunk, K then V, into one stage of its ring; and its part of the queries of a unit
@@ -699,13 +698,18 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 2)) k_paged_attn_mm
 }
 
 // ---- fp32: CUDA cores ----------------------------------------------------------------------------------------------------
-// Scores: a lane takes one slot and half of the dimensions; P V: a lane takes DH / 32 dimensions.  A kernel for every power of two of
-// rows: the work a slot costs goes with the rows, and a branch a row and slot (16 of them with one real row) took ten times the bytes' time.
+// With more than a row or two the time is shared memory's: a 16-byte load of a warp takes four cycles, in which the SM has 16 FMAs a lane, so a
+// lane's tile of the products has to be wide both ways.  Scores: eight lanes of each slot, a quarter of the slots a lane, so that 4 + NR
+// loads feed 16 NR FMAs; the eight lanes' sums are then scattered, NR / 2 (row, slot)s each, and the softmax is done there, once.  P V:
+// a lane takes DH / 32 dimensions of all rows; the weights reach it through the K rows' place, which nobody reads any more.
+// A kernel for every power of two of rows: the work a slot costs goes with the rows.
 template <int DH, int NR, bool A16>
 __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 4)) k_paged_attn_simt(const PagedAttnArgs a) {
   extern __shared__ __align__(128) char pa_smem[];
   constexpr int VEC = DH / 32;                  // dimensions of a lane in P V
-  constexpr int PARTS = NR <= 2 ? 4 : 1;        // independent sums of a score (few rows: the chain of FMAs would be the time)
+  constexpr int OWN = NR >= 2 ? NR / 2 : 1;     // (row, slot)s of a lane in the softmax: RO rows of KO slots
+  constexpr int RO = NR == 16 ? 2 : 1, KO = OWN / RO;
+  constexpr int SHARE = NR >= 8 ? 0 : 8 / NR - 1;       // the bits of a lane in which those that share a row differ, besides 8 and 16
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   int* pre = reinterpret_cast<int*>(pa_smem + PaSmem<float, DH>::pre(a.q_rows, a.merge_rows));
   pdl_release();
@@ -723,19 +727,24 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 4)) k_paged_attn_si
   if (threadIdx.x < 2) cut[threadIdx.x].p.left = 0;
 
   PaRing<float, DH, A16> ring(a, pre, hi, p, pa_smem);
-  const int key = lane & 15, half = lane >> 4;
+  // slots kq + 4 i; of their rows' 16-byte chunks those with d as their lower bits; in the softmax rows r0 .. of slots kq + 4 (i0 ..)
+  const int kq = lane >> 3, d = lane & 7;
+  const int r0 = NR == 16 ? 2 * d : NR == 1 ? 0 : d * NR / 8, i0 = NR >= 8 ? 0 : NR == 1 ? d >> 1 : d * OWN % 4;
   for (; p.left > 0; p = pa_place(a, pre, p.next(), hi)) {
     const RowSpan rs = pg_rows(a.pv, a.row_off, p.b, a.max_rows, a.n_rows);
     const int nr = min(PA_ROWS, rs.n * a.group - p.rt * PA_ROWS);
-    float o[NR][VEC], m[NR], l[NR];             // m: the same in all lanes; l: this lane's slots
+    float o[NR][VEC], m[RO], l[RO];             // m: the same in all lanes that share the row; l: this lane's slots
 #pragma unroll
-    for (int r = 0; r < NR; ++r) {
-      m[r] = -INFINITY;
-      l[r] = 0.f;
+    for (int r = 0; r < NR; ++r)
 #pragma unroll
       for (int e = 0; e < VEC; ++e) o[r][e] = 0.f;
+#pragma unroll
+    for (int r = 0; r < RO; ++r) {
+      m[r] = -INFINITY;
+      l[r] = 0.f;
     }
     const char* qs = nullptr;
+#pragma unroll 1
     for (int k = 0; k < p.left; ++k) {
       char* rows;
       const unsigned mask = ring.turn(rows);
@@ -743,64 +752,130 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 4)) k_paged_attn_si
         __syncthreads();
         qs = ring.queries();
       }
-      const int j = (p.chunk + k) * PA_CHUNK + w * 16 + key;
-      if (mask == 0 && (!a.scores || j - key >= p.len)) continue;
-      const char* ks = rows;
-      const char* vs = ks + 16 * DH * 4;
-      float s[NR][PARTS];
+      const int j0 = (p.chunk + k) * PA_CHUNK + w * 16;
+      if (mask == 0 && (!a.scores || j0 >= p.len)) continue;
+      const char* vs = rows + 16 * DH * 4;
+      float s[4 * NR];                          // [row][i]
 #pragma unroll
-      for (int r = 0; r < NR; ++r)
+      for (int x = 0; x < 4 * NR; ++x) s[x] = 0.f;
 #pragma unroll
-        for (int x = 0; x < PARTS; ++x) s[r][x] = 0.f;
-#pragma unroll 4
-      for (int ch = 0; ch < DH / 8; ++ch) {
-        const float4 kv = *reinterpret_cast<const float4*>(ks + pa_at<float, DH>(key, half * (DH / 8) + ch));
+      for (int ch = 0; ch < DH / 32; ++ch) {
+        float4 kv[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kv[i] = *reinterpret_cast<const float4*>(rows + pa_at<float, DH>(kq + 4 * i, ch * 8 + d));
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
-          const float4 qv = *reinterpret_cast<const float4*>(qs + pa_q_at<float, DH>(r < nr ? r : 0, half * (DH / 8) + ch));
-          float& x = s[r][ch % PARTS];
-          x = fmaf(qv.x, kv.x, fmaf(qv.y, kv.y, fmaf(qv.z, kv.z, fmaf(qv.w, kv.w, x))));
+          const float4 qv = *reinterpret_cast<const float4*>(qs + pa_q_at<float, DH>(r, ch * 8 + d));    // (r >= nr: what lies there; nobody reads its sums)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float& x = s[r * 4 + i];
+            x = fmaf(qv.x, kv[i].x, fmaf(qv.y, kv[i].y, fmaf(qv.z, kv[i].z, fmaf(qv.w, kv[i].w, x))));
+          }
         }
       }
-      float pr[NR];
+      // the eight lanes' sums: halves are exchanged until each lane has its OWN ones
 #pragma unroll
-      for (int r = 0; r < NR; ++r) {
-        float x = PARTS == 4 ? (s[r][0] + s[r][1 % PARTS]) + (s[r][2 % PARTS] + s[r][3 % PARTS]) : s[r][0];
-        x += __shfl_xor_sync(0xffffffffu, x, 16);
-        x = (mask >> key) & 1 ? x * a.scale_log2 : -INFINITY;
-        if (a.scores && half == 0 && j < p.len && r < nr) {
+      for (int b = 4, n = 4 * NR; b >= 1; b >>= 1) {
+        if (n > 1) {
+          n >>= 1;
+          const bool up = (d & b) != 0;
+#pragma unroll
+          for (int x = 0; x < 2 * NR; ++x)
+            if (x < n) {
+              const float give = up ? s[x] : s[x + n], keep = up ? s[x + n] : s[x];
+              s[x] = keep + __shfl_xor_sync(0xffffffffu, give, b);
+            }
+        } else {
+          s[0] += __shfl_xor_sync(0xffffffffu, s[0], b);
+        }
+      }
+      __syncwarp();                             // the K rows have been read: the weights [slot][row] take their place
+      float* ps = reinterpret_cast<float*>(rows);
+      float corr[RO], pr[RO][KO];
+      bool raised = false;
+#pragma unroll
+      for (int r = 0; r < RO; ++r) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < KO; ++i) {
+          float& x = s[r * KO + i];
+          x = (mask >> (kq + 4 * (i0 + i))) & 1 ? x * a.scale_log2 : -INFINITY;
+          top = fmaxf(top, x);
+        }
+        if (a.scores && r0 + r < nr) {
           int row, head;
-          pa_row(a, rs, p, r, row, head);
-          a.scores[((long long)row * a.hq + head) * pg_capacity(a.pv) + j] = x;
-        }
-        const float m_new = fmaxf(m[r], warp_max(x));
-        const float corr = pa_scale(m[r], m_new);
-        m[r] = m_new;
-        pr[r] = x == -INFINITY ? 0.f : pa_exp2(x - m_new);
-        l[r] = l[r] * corr + pr[r];
+          pa_row(a, rs, p, r0 + r, row, head);
+          float* dst = a.scores + ((long long)row * a.hq + head) * pg_capacity(a.pv);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) o[r][e] *= corr;
+          for (int i = 0; i < KO; ++i) {
+            const int j = j0 + kq + 4 * (i0 + i);
+            if (j < p.len) dst[j] = s[r * KO + i];
+          }
+        }
+#pragma unroll
+        for (int b = 1; b < 32; b <<= 1)
+          if (b >= 8 || (SHARE & b)) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, b));
+        // (a maximum that rises by little is left: the weights are then at most 2^PA_LAZY)
+        corr[r] = 1.f;
+        if (top > m[r] + PA_LAZY) {
+          corr[r] = pa_scale(m[r], top);
+          m[r] = top;
+          raised = true;
+        }
+        l[r] *= corr[r];
+#pragma unroll
+        for (int i = 0; i < KO; ++i) {
+          const float x = s[r * KO + i];
+          pr[r][i] = x == -INFINITY ? 0.f : pa_exp2(x - m[r]);
+          l[r] += pr[r][i];
+        }
       }
+#pragma unroll
+      for (int i = 0; i < KO; ++i) {
+        float* dst = ps + (kq + 4 * (i0 + i)) * NR + r0;
+        if constexpr (RO == 2) *reinterpret_cast<float2*>(dst) = make_float2(pr[0][i], pr[1][i]);
+        else *dst = pr[0][i];
+      }
+      if (__any_sync(0xffffffffu, raised)) {
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+          const float c = __shfl_sync(0xffffffffu, corr[r % RO], NR == 16 ? r / 2 : r * 8 / NR);
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) o[r][e] *= c;
+        }
+      }
+      __syncwarp();
 #pragma unroll 4
       for (int i = 0; i < 16; ++i) {
-        float v[VEC];
+        float v[VEC], x[NR];
         if constexpr (VEC == 4) {
-          const float4 x = *reinterpret_cast<const float4*>(vs + pa_at<float, DH>(i, lane));
-          v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+          const float4 y = *reinterpret_cast<const float4*>(vs + pa_at<float, DH>(i, lane));
+          v[0] = y.x; v[1] = y.y; v[2] = y.z; v[3] = y.w;
         } else {
-          const float2 x = *reinterpret_cast<const float2*>(vs + pa_at<float, DH>(i, lane >> 1) + (lane & 1) * 8);
-          v[0] = x.x; v[1] = x.y;
+          const float2 y = *reinterpret_cast<const float2*>(vs + pa_at<float, DH>(i, lane >> 1) + (lane & 1) * 8);
+          v[0] = y.x; v[1] = y.y;
+        }
+        if constexpr (NR >= 4) {
+#pragma unroll
+          for (int r = 0; r < NR; r += 4) {
+            const float4 y = *reinterpret_cast<const float4*>(ps + i * NR + r);
+            x[r] = y.x; x[r + 1] = y.y; x[r + 2] = y.z; x[r + 3] = y.w;
+          }
+        } else {
+#pragma unroll
+          for (int r = 0; r < NR; ++r) x[r] = ps[i * NR + r];
         }
 #pragma unroll
-        for (int r = 0; r < NR; ++r) {
-          const float x = __shfl_sync(0xffffffffu, pr[r], i);
+        for (int r = 0; r < NR; ++r)
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) o[r][e] = fmaf(x, v[e], o[r][e]);
-        }
+          for (int e = 0; e < VEC; ++e) o[r][e] = fmaf(x[r], v[e], o[r][e]);
       }
     }
 #pragma unroll
-    for (int r = 0; r < NR; ++r) l[r] = warp_sum(half == 0 ? l[r] : 0.f);
+    for (int r = 0; r < RO; ++r)
+#pragma unroll
+      for (int b = 1; b < 32; b <<= 1)
+        if (b >= 8 || (SHARE & b & (NR == 1 ? 6 : 7))) l[r] += __shfl_xor_sync(0xffffffffu, l[r], b);     // (one row: two lanes have each slot)
     pa_finish<float, DH>(a, deal, p, rs, lo, cut, pa_smem, [&](int i0, int n, float* dst, float2* ml) {
 #pragma unroll
       for (int r = 0; r < NR; ++r) {
@@ -808,7 +883,7 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 4)) k_paged_attn_si
         if (i < 0 || i >= n) continue;
 #pragma unroll
         for (int e = 0; e < VEC; e += 2) *reinterpret_cast<float2*>(dst + i * DH + (((lane * VEC + e) / 2) ^ (4 * i)) * 2) = make_float2(o[r][e], o[r][e + 1]);
-        if (lane == 0) ml[i] = make_float2(m[r], l[r]);
+        if (lane == (NR == 16 ? r / 2 : r * 8 / NR)) ml[i] = make_float2(m[r % RO], l[r % RO]);
       }
     });
   }
