@@ -528,7 +528,7 @@ __device__ __forceinline__ void pa_join(const PagedAttnArgs& a, const PaCut* cut
 // Rows of sequences without a slot: 0.  (The grid's CTAs take the sequences in turn.)
 template <typename T, int DH>
 __device__ __forceinline__ void pa_empty(const PagedAttnArgs& a, const int* pre) {
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int w = threadIdx.x >> 5;
   for (int b = blockIdx.x; b < a.pv.batch; b += gridDim.x) {
     if (pre[b + 1] > pre[b]) continue;
     const RowSpan rs = pg_rows(a.pv, a.row_off, b, a.max_rows, a.n_rows);
@@ -698,10 +698,12 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 2)) k_paged_attn_mm
 }
 
 // ---- fp32: CUDA cores ----------------------------------------------------------------------------------------------------
-// With more than a row or two the time is shared memory's: a 16-byte load of a warp takes four cycles, in which the SM has 16 FMAs a lane, so a
-// lane's tile of the products has to be wide both ways.  Scores: eight lanes of each slot, a quarter of the slots a lane, so that 4 + NR
-// loads feed 16 NR FMAs; the eight lanes' sums are then scattered, NR / 2 (row, slot)s each, and the softmax is done there, once.  P V:
-// a lane takes DH / 32 dimensions of all rows; the weights reach it through the K rows' place, which nobody reads any more.
+// A lane's tile of the products is wide both ways, since a 16-byte load of shared memory takes a warp as long as 16 FMAs or more.  Scores: eight
+// lanes of each slot, a quarter of the slots a lane, so that 4 + NR loads feed 16 NR FMAs; the eight lanes' sums are then scattered, NR / 2
+// (row, slot)s each, and the softmax is done there, once.  P V: a lane takes DH / 32 dimensions of all rows; the weights reach it through
+// the K rows' place, which nobody reads any more.  (One slot and half of the dimensions a lane, the weights by a shuffle each: 4 x 4000 slots of 32
+// heads of 128, 1 / 4 / 8 rows 72 / 98 / 158 us, so 70 / 74 / 88; 67 are the bytes.)  Sixteen rows of 128 are bound by the latency of the four
+// warps that an SM's registers and rings leave.
 // A kernel for every power of two of rows: the work a slot costs goes with the rows.
 template <int DH, int NR, bool A16>
 __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 4)) k_paged_attn_simt(const PagedAttnArgs a) {
@@ -709,6 +711,10 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 4)) k_paged_attn_si
   constexpr int VEC = DH / 32;                  // dimensions of a lane in P V
   constexpr int OWN = NR >= 2 ? NR / 2 : 1;     // (row, slot)s of a lane in the softmax: RO rows of KO slots
   constexpr int RO = NR == 16 ? 2 : 1, KO = OWN / RO;
+  // Loops as long as the instruction cache holds: sixteen rows of 128 (16 x 12000 slots of 4 heads, groups of 7) 185 us, unrolled as fewer rows are 297;
+  // eight rows 111, as short as sixteen's 123.
+  constexpr bool LONG = NR * DH == 16 * 128;
+  constexpr int UNROLL_S = LONG ? 1 : DH / 32, UNROLL_O = LONG ? 4 : 8;
   constexpr int SHARE = NR >= 8 ? 0 : 8 / NR - 1;       // the bits of a lane in which those that share a row differ, besides 8 and 16
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   int* pre = reinterpret_cast<int*>(pa_smem + PaSmem<float, DH>::pre(a.q_rows, a.merge_rows));
@@ -758,7 +764,7 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 4)) k_paged_attn_si
       float s[4 * NR];                          // [row][i]
 #pragma unroll
       for (int x = 0; x < 4 * NR; ++x) s[x] = 0.f;
-#pragma unroll
+#pragma unroll UNROLL_S
       for (int ch = 0; ch < DH / 32; ++ch) {
         float4 kv[4];
 #pragma unroll
@@ -845,7 +851,7 @@ __global__ void __launch_bounds__(PA_THREADS, pa_ctas_sm(DH, 4)) k_paged_attn_si
         }
       }
       __syncwarp();
-#pragma unroll 4
+#pragma unroll UNROLL_O
       for (int i = 0; i < 16; ++i) {
         float v[VEC], x[NR];
         if constexpr (VEC == 4) {

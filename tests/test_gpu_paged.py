@@ -109,6 +109,31 @@ def test_scales_from_flat_to_one_hot(scale, q_scale):
     _check_attention(U.Pool([500, 77], MHA, BF, 16), [1, 1], False, scale=scale, q_scale=q_scale)
 
 
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("group", [1, 2, 3, 4, 5, 8, 9, 16, 17])
+@pytest.mark.parametrize("scale,q_scale", [(None, 2.0), (1.0, 6.0)])
+def test_fp32_groups_of_all_sizes(group, dh, scale, q_scale):
+    """A kernel for each power of two of rows, full and not; maxima that rise late and far, too."""
+    _check_attention(U.Pool([1, 77, 0, 640], (2 * group, 2, dh), F32, 16), [1] * 4, False, scale=scale, q_scale=q_scale, seed=group)
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("group", [1, 2, 4, 8, 16])
+def test_fp32_infinite_and_nan_rows_stay_with_their_head(group, dh):
+    pool = U.Pool([100, 100], (4 * group, 4, dh), F32, 16)
+    b0 = pool.table[0].long()
+    pool.v[b0[1], 3, 2] = float("nan")
+    pool.k[b0[2], 3, 1, 0] = float("inf")
+    pool.k[b0[6], 4:, 3] = float("nan")            # the last page's slots behind the sequence
+    pool.v[b0[6], 4:, 3] = float("nan")
+    q = torch.rand(2, 4 * group * dh, device=DEV) + 0.5
+    out = torch.empty_like(q)
+    _cache(pool).attention(q, pool.lens, out)
+    out = out.view(2, 4, group * dh)
+    assert bool(out[0, 2].isnan().all()) and bool(out[0, 1].isnan().all())
+    assert bool(out[0, 0].isfinite().all()) and bool(out[0, 3].isfinite().all()) and bool(out[1].isfinite().all())
+
+
 def test_without_weights_the_same_bits():
     pool = U.Pool([700, 3, 64], GQA, BF, 16)
     a = _check_attention(pool, [1, 1, 1], False, weights=True)
