@@ -375,6 +375,8 @@ class PagedKVCache:
     at most n_rows packed rows, by default max_rows for every sequence; with `weights` for attention that gathers them) and the status
     word that check() reads.  Calls of one object must not overlap on the device: give each stream, and each captured graph that may run
     beside others, an object of its own over the same pools.  Every call enqueues on the current stream of the pools' device, or on `stream`.
+    An object is ready for any stream once it is made (the constructor waits for its stream).  One made in a stream capture belongs to that graph: its
+    calls are those of the capture, and others raise.
     """
 
     def __init__(self, k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: Optional[torch.Tensor] = None, *, n_heads: int,
@@ -420,6 +422,16 @@ class PagedKVCache:
         self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
         self.workspace[:4096].zero_()          # arrival counters
         self._ws, self._ws_bytes = self.workspace.data_ptr(), need
+        # Counters and status are clear ahead of any call, whatever stream it takes: waited for here; in a capture, which forbids that, by each
+        # further stream of it.
+        made_on = torch.cuda.current_stream(self.device)
+        self._streams, self._cleared = {made_on.cuda_stream}, None
+        with torch.cuda.device(self.device):
+            if torch.cuda.is_current_stream_capturing():
+                self._cleared = torch.cuda.Event()
+                self._cleared.record(made_on)
+            else:
+                made_on.synchronize()
 
     # (the checks run with every call of a few microseconds: each is one comparison of what torch hands out as it is)
     def _tensor(self, name, t, dtype, shape):
@@ -449,8 +461,16 @@ class PagedKVCache:
         if rc != 0:
             raise LSPError(rc, self._err.value.decode())
 
+    def _meet(self, stream, sptr):
+        """Ahead of the first call on a stream that the object was not made on."""
+        if self._cleared is not None:
+            (torch.cuda.current_stream(self.device) if stream is None else stream).wait_event(self._cleared)
+        self._streams.add(sptr)
+
     def _call(self, stream, fn, *args):
         sptr = torch._C._cuda_getCurrentRawStream(self._index) if stream is None else stream.cuda_stream
+        if sptr not in self._streams:
+            self._meet(stream, sptr)
         if torch._C._cuda_getDevice() == self._index:
             rc = fn(self._ref, *args, sptr, self._err, 256)
         else:

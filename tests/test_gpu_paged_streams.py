@@ -1,0 +1,81 @@
+"""The paged key-value cache on streams other than the one its object was made on: counters and status word are clear before any call."""
+import pytest
+import torch
+
+import paged_util as U
+from gpu_util import DEV
+
+pytestmark = pytest.mark.gpu
+
+BF = torch.bfloat16
+HEADS = (8, 2, 64)
+
+
+def _pool():
+    return U.Pool([3000, 1200], HEADS, BF, 16)             # long enough that runs cut units: parts are joined
+
+
+def _object(pool):
+    from paper_2603_05454_b200 import PagedKVCache
+    return PagedKVCache(pool.k, pool.v, pool.table, n_heads=HEADS[0], weights=True)
+
+
+def _want(pool, q):
+    out = torch.empty_like(q)
+    _object(pool).attention(q, pool.lens, out)
+    torch.cuda.synchronize()
+    return out
+
+
+def _dirty(n):
+    """Memory that the allocator hands out next holds no zeros."""
+    for size in (n, 1):
+        torch.full((size,), 0xFF, dtype=torch.uint8, device=DEV)
+    torch.full((1,), -1, dtype=torch.int32, device=DEV)
+
+
+@pytest.mark.parametrize("how", ["argument", "current"])
+def test_a_call_on_another_stream_right_after_the_construction(how):
+    pool = _pool()
+    q = torch.randn(2, HEADS[0] * 64, device=DEV).to(BF)
+    want, out, side = _want(pool, q), torch.zeros_like(q), torch.cuda.Stream()
+    _dirty(_object(pool).workspace.numel())
+    torch.cuda.synchronize()
+    torch.cuda._sleep(400_000_000)                          # the stream of the construction is a fifth of a second behind
+    c = _object(pool)
+    if how == "argument":
+        c.attention(q, pool.lens, out, stream=side)
+    else:
+        with torch.cuda.stream(side):
+            c.attention(q, pool.lens, out)
+    side.synchronize()
+    got = out.clone()
+    torch.cuda.synchronize()
+    c.attention(q, pool.lens, out)                          # and the counters are clear behind it
+    c.check()
+    assert torch.equal(got, want) and torch.equal(out, want)
+
+
+def test_an_object_made_in_a_capture_is_the_graphs_own():
+    """Its clears are replayed with the graph, ahead of the calls on every stream of the capture; an eager call is an error, not a wrong result."""
+    pool = _pool()
+    q = torch.randn(2, HEADS[0] * 64, device=DEV).to(BF)
+    want, outs, graph, side = _want(pool, q), [torch.zeros_like(q) for _ in range(2)], torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        main = torch.cuda.current_stream()
+        side.wait_stream(main)                              # forked ahead of the construction
+        c = _object(pool)
+        c.attention(q, pool.lens, outs[0], stream=side)
+        main.wait_stream(side)
+        c.attention(q, pool.lens, outs[1])
+    for _ in range(3):
+        for o in outs:
+            o.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], want) and torch.equal(outs[1], want)
+    with pytest.raises(RuntimeError):
+        c.attention(q, pool.lens, outs[0])
+    torch.cuda.synchronize()
+    del graph, c
