@@ -376,7 +376,8 @@ class PagedKVCache:
     word that check() reads.  Calls of one object must not overlap on the device: give each stream, and each captured graph that may run
     beside others, an object of its own over the same pools.  Every call enqueues on the current stream of the pools' device, or on `stream`.
     An object is ready for any stream once it is made (the constructor waits for its stream).  One made in a stream capture belongs to that graph: its
-    calls are those of the capture, and others raise.
+    calls are those of the capture, and others raise.  It may be dropped while calls on torch's streams are still running; keep it for those on an
+    external stream, and for the replays of a graph that holds its calls.
     """
 
     def __init__(self, k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: Optional[torch.Tensor] = None, *, n_heads: int,
@@ -463,8 +464,15 @@ class PagedKVCache:
 
     def _meet(self, stream, sptr):
         """Ahead of the first call on a stream that the object was not made on."""
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device)
         if self._cleared is not None:
-            (torch.cuda.current_stream(self.device) if stream is None else stream).wait_event(self._cleared)
+            stream.wait_event(self._cleared)
+        # The allocator gives the object's memory out again only behind what the stream has been handed by then.  (Not a stream that torch did not
+        # make, whose id is its address: it may be gone by then, and the allocator would still ask it.)
+        if isinstance(stream, torch.cuda.Stream) and (sptr == 0 or stream.stream_id != sptr):
+            self.workspace.record_stream(stream)
+            self.status.record_stream(stream)
         self._streams.add(sptr)
 
     def _call(self, stream, fn, *args):

@@ -1,4 +1,5 @@
-"""The paged key-value cache on streams other than the one its object was made on: counters and status word are clear before any call."""
+"""The paged key-value cache on streams other than the one its object was made on: counters and status word are clear before any call, and the
+object's own memory is not given out again under a call that is still running."""
 import pytest
 import torch
 
@@ -54,6 +55,40 @@ def test_a_call_on_another_stream_right_after_the_construction(how):
     c.attention(q, pool.lens, out)                          # and the counters are clear behind it
     c.check()
     assert torch.equal(got, want) and torch.equal(out, want)
+
+
+def test_memory_of_a_dropped_object_waits_for_its_calls():
+    pool = _pool()
+    q = torch.randn(2, HEADS[0] * 64, device=DEV).to(BF)
+    want, out, side = _want(pool, q), torch.zeros_like(q), torch.cuda.Stream()
+    c = _object(pool)
+    at, status, n = c.workspace.data_ptr(), c.status.data_ptr(), c.workspace.numel()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(400_000_000)
+    c.attention(q, pool.lens, out, stream=side)
+    del c
+    taken = [torch.full((n,), 0xFF, dtype=torch.uint8, device=DEV), *(torch.full((1,), -1, dtype=torch.int32, device=DEV) for _ in range(4))]
+    assert all(t.data_ptr() not in (at, status) for t in taken)
+    side.synchronize()
+    assert torch.equal(out, want) and all(bool((t == (255 if t.dtype == torch.uint8 else -1)).all()) for t in taken)
+
+
+def test_a_stream_from_outside_torch_may_be_gone_before_the_object():
+    import ctypes as C
+    cuda = C.CDLL("libcudart.so.12")
+    handle, pool = C.c_void_p(), _pool()
+    q = torch.randn(2, HEADS[0] * 64, device=DEV).to(BF)
+    want, out = _want(pool, q), torch.zeros_like(q)
+    assert cuda.cudaStreamCreateWithFlags(C.byref(handle), 1) == 0
+    c = _object(pool)
+    torch.cuda.synchronize()
+    c.attention(q, pool.lens, out, stream=torch.cuda.ExternalStream(handle.value))
+    assert cuda.cudaStreamSynchronize(handle) == 0 and torch.equal(out, want)
+    assert cuda.cudaStreamDestroy(handle) == 0
+    n = c.workspace.numel()
+    del c
+    assert bool((torch.full((n,), 3, dtype=torch.uint8, device=DEV) == 3).all())
 
 
 def test_an_object_made_in_a_capture_is_the_graphs_own():
