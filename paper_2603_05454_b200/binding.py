@@ -532,6 +532,7 @@ class PagedKVCache:
         bits = int(self.status.item())
         if bits:
             self.status.zero_()
+            torch.cuda.synchronize(self.device)        # (ahead of the next call, on whatever stream)
             words = [w for bit, w in ((PAGED_BAD_LEN, "a length outside the sequence's pages"), (PAGED_BAD_PAGE, "a table entry outside the pool"),
                                       (PAGED_BAD_ROWS, "row offsets out of range")) if bits & bit]
             raise LSPError(-4, f"paged cache: {', '.join(words)} (status {bits})")

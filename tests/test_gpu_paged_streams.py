@@ -74,6 +74,34 @@ def test_memory_of_a_dropped_object_waits_for_its_calls():
     assert torch.equal(out, want) and all(bool((t == (255 if t.dtype == torch.uint8 else -1)).all()) for t in taken)
 
 
+def test_a_status_that_was_raised_is_clear_for_the_next_call_on_any_stream():
+    from paper_2603_05454_b200 import LSPError
+    pool = _pool()
+    q = torch.randn(2, HEADS[0] * 64, device=DEV).to(BF)
+    out, side, bad = torch.zeros_like(q), torch.cuda.Stream(), pool.lens + pool.cap
+    c = _object(pool)
+    word = c.status
+
+    class Late:
+        """The status word, cleared on a stream that is a fifth of a second behind."""
+        item = word.item
+
+        def zero_(self):
+            torch.cuda._sleep(400_000_000)
+            word.zero_()
+
+    torch.cuda.synchronize()
+    c.attention(q, bad, out)
+    c.status = Late()
+    with pytest.raises(LSPError):
+        c.check()
+    c.status = word
+    c.attention(q, bad, out, stream=side)
+    with pytest.raises(LSPError):
+        c.check()
+    c.check()
+
+
 def test_a_stream_from_outside_torch_may_be_gone_before_the_object():
     import ctypes as C
     cuda = C.CDLL("libcudart.so.12")
