@@ -274,7 +274,8 @@ int lsp_linear_static(const void* A, const void* W, void* out, int M, int N, int
  * or an append past it (clamped); bit 2 = a table entry outside [0, n_pages) for a slot in use (the slot is not read or written and gets
  * no weight; a pair of slots of an eviction is not moved); bit 4 = row offsets that descend, leave [0, n_rows] or span more
  * than max_rows (that sequence has no rows then).  Nothing outside the given buffers is touched in any of these cases, and the
- * other sequences' results hold.  err, err_len: optional host buffer for the message of a failing call.
+ * other sequences' results hold (where offsets descend in such a way that two of them name a row, it is appended to both; its attention is one of
+ * theirs, and their weights are undefined).  err, err_len: optional host buffer for the message of a failing call.
  * Limits: head_dim 64 or 128, batch <= 1024, n_kv_heads <= 1024, max_pages * page_size <= 2^20, every pointer and stride of T a
  * multiple of 16 bytes. */
 typedef struct {

@@ -27,8 +27,38 @@ struct PagedAppendArgs {
   int* pos;
 };
 
-// Blocks ahead of the last: rows_block packed rows each.  The last block: the lengths.
-__global__ void __launch_bounds__(PP_THREADS) k_paged_append(const PagedAppendArgs a) {
+// All rows of a call whose offsets descend somewhere (so there are bad ones), by one block, a sequence with good offsets after another.  Such offsets
+// cannot be searched: the other blocks' search for a row's sequence misses rows, and the good offsets may name a row more than once.  (What the
+// others do write is right, and the same.)
+__device__ __forceinline__ void pp_any_order(const PagedAppendArgs& a) {
+  const int cap = pg_capacity(a.pv), head_pieces = a.head_bytes / 16, pieces = a.pv.hkv * head_pieces;
+#pragma unroll 1
+  for (int b = 0; b < a.pv.batch; ++b) {
+    const RowSpan rs = pg_rows(a.pv, a.row_off, b, a.max_rows, a.n_rows);
+    const int len = pg_len(a.pv, a.lens[b]);
+#pragma unroll 1
+    for (int r = 0; r < min(rs.n, cap - len); ++r) {
+      const long long at = pg_slot(a.pv, b, len + r);
+      if (at < 0) continue;
+#pragma unroll 1
+      for (int c = threadIdx.x; c < 2 * pieces; c += PP_THREADS) {
+        const int v = c >= pieces ? 1 : 0, p = c - v * pieces, h = p / head_pieces;
+        char* dst = (v ? a.pv.v : a.pv.k) + (at + (long long)h * a.pv.head_stride) * a.esz + (p - h * head_pieces) * 16;
+        *reinterpret_cast<uint4*>(dst) = reinterpret_cast<const uint4*>((v ? a.v_new : a.k_new) + (long long)(rs.first + r) * a.ld_new)[p];
+      }
+#pragma unroll 1
+      for (int h = threadIdx.x; h < a.pv.hkv; h += PP_THREADS) {
+        const long long x = ((long long)b * a.pv.hkv + h) * cap + len + r;
+        if (a.weights) a.weights[x] = 0.f;
+        if (a.pos) a.pos[x] = a.seen ? a.seen[b] + r : len + r;
+      }
+    }
+  }
+}
+
+// Blocks ahead of the last: rows_block packed rows each.  The last block: the lengths, and what the others miss where offsets descend.
+// (Five blocks an SM, 48 registers: with 40 16 x 1000 rows of 512 bytes took 6.2 us, with 64 7.4, so 5.6.)
+__global__ void __launch_bounds__(PP_THREADS, 5) k_paged_append(const PagedAppendArgs a) {
   extern __shared__ int offsets[];      // [batch] row_off, [batch] lens (with offsets: a row's sequence is searched for)
   __shared__ int seqs[PP_ROWS], slots[PP_ROWS], poss[PP_ROWS];
   __shared__ long long places[PP_ROWS]; // bytes, -1: nowhere
@@ -38,6 +68,7 @@ __global__ void __launch_bounds__(PP_THREADS) k_paged_append(const PagedAppendAr
   pg_prefetch(a.lens, B * 4, threadIdx.x * gridDim.x + blockIdx.x, gridDim.x * PP_THREADS);
   pdl_wait();
   if (blockIdx.x == gridDim.x - 1) {
+    bool descend = false;
     for (int b = threadIdx.x; b < B; b += PP_THREADS) {
       const RowSpan rs = pg_rows(a.pv, a.row_off, b, a.max_rows, a.n_rows);
       const int n = pg_len(a.pv, a.lens[b]);
@@ -48,7 +79,9 @@ __global__ void __launch_bounds__(PP_THREADS) k_paged_append(const PagedAppendAr
       }
       a.lens_out[b] = n + fit;
       if (a.seen_out) a.seen_out[b] = a.seen[b] + fit;
+      descend |= a.row_off && a.row_off[b] > a.row_off[b + 1];
     }
+    if (a.row_off && __syncthreads_or(descend)) pp_any_order(a);
     return;
   }
   const int r0 = blockIdx.x * a.rows_block, n = min(a.rows_block, a.n_rows - r0);
