@@ -299,8 +299,11 @@ __device__ __forceinline__ void pe_move(const PagedEvictArgs& a, int unit, const
     for (int i = 0; i < PM_PAIRS; ++i)
       if (to[i] >= 0 && c0 < a.head_bytes) x[i] = *reinterpret_cast<const uint4*>(pool + from[i] + c0);
     const bool mine = lane < PM_PAIRS && j >= 0 && to_slot >= 0;
-    const float weight = mine ? a.weights[base + j] : 0.f;
-    const int p = mine && a.pos ? a.pos[base + j] : j;
+    float weight = mine ? a.weights[base + j] : 0.f;
+    int p = mine && a.pos ? a.pos[base + j] : j;
+    bool moved = true;
+#pragma unroll
+    for (int i = 0; i < PM_PAIRS; ++i) moved = lane == i ? to[i] >= 0 : moved;
     const int j3 = slot(i0 + 2 * step);
     const long long off2 = offset(j2);
 #pragma unroll
@@ -313,6 +316,10 @@ __device__ __forceinline__ void pe_move(const PagedEvictArgs& a, int unit, const
 #pragma unroll
       for (int i = 0; i < PM_PAIRS; ++i)
         if (to[i] >= 0) *reinterpret_cast<uint4*>(pool + to[i] + c0 + 256) = x[i];
+    }
+    if (mine && !moved) {                            // a slot of the pair has no page: the one ahead keeps what is in it
+      weight = a.weights[base + to_slot];
+      p = a.pos ? a.pos[base + to_slot] : to_slot;
     }
     if (mine) {
       a.weights_out[base + to_slot] = weight;
