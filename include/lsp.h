@@ -274,8 +274,8 @@ int lsp_linear_static(const void* A, const void* W, void* out, int M, int N, int
  * or an append past it (clamped); bit 2 = a table entry outside [0, n_pages) for a slot in use (the slot is not read or written and gets
  * no weight; a pair of slots of an eviction is not moved, and the slot ahead of the budget keeps its own weight and position); bit 4 = row offsets that descend, leave [0, n_rows] or span more
  * than max_rows (that sequence has no rows then).  Nothing outside the given buffers is touched in any of these cases, and the
- * other sequences' results hold (where offsets descend in such a way that two of them name a row, it is appended to both; its attention is one of
- * theirs, and their weights are undefined).  err, err_len: optional host buffer for the message of a failing call.
+ * other sequences' results hold (where offsets descend in such a way that two of them name a row, it is appended to both, and its attention
+ * and their weights are undefined).  err, err_len: optional host buffer for the message of a failing call.
  * Limits: head_dim 64 or 128, batch <= 1024, n_kv_heads <= 1024, max_pages * page_size <= 2^20, every pointer and stride of T a
  * multiple of 16 bytes. */
 typedef struct {
@@ -325,7 +325,8 @@ int lsp_paged_attention(const lsp_paged_kv* kv, const void* q, long long ldq, in
  * slot's weight and position to weights_out and pos_out.  Which slot holds a key carries no meaning for attention (keys are
  * rotated already); pos_out says which position it is, per KV head.  Sequences of at most budget slots keep theirs.
  *   weights, pos        device [batch][n_kv_heads][max_pages * page_size]; pos NULL: the slot (pos_out may be NULL then)
- *   lens, seen          device [batch]; seen NULL: lens
+ *   lens, seen          device [batch]; seen NULL: lens, which is right up to the first eviction only: from then on a sequence has seen more positions than
+ *                       it has slots, and without seen ever more of them count as recent, until the newest are dropped in favour of older ones
  *   weights_out, pos_out, lens_out   as the inputs, not overlapping them; lens_out = min(lens, budget); slots behind it are not written
  * Pages behind ceil(lens_out / page_size) are free afterwards.  The pages of a sequence that is thinned must belong to it alone.
  * workspace: lsp_paged_evict_workspace() bytes, aligned as above; the attention's may be taken (its counters are left alone). */

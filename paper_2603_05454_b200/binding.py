@@ -518,7 +518,8 @@ class PagedKVCache:
 
     def evict(self, weights: torch.Tensor, lens: torch.Tensor, budget: int, weights_out: torch.Tensor, lens_out: torch.Tensor, *,
               n_sink: int = 0, n_recent: int = 0, pos=None, pos_out=None, seen=None, stream=None):
-        """Thins every sequence to at most budget slots per KV head (lsp_paged_evict)."""
+        """Thins every sequence to at most budget slots per KV head (lsp_paged_evict).  seen: positions of each sequence so far (the append's seen_out);
+        needed with n_recent for a sequence that was thinned before, since without it the number of slots is taken, and positions lie beyond that."""
         i32, f32, b, slots, tensor = torch.int32, torch.float32, self._per_seq, self._per_slot, self._tensor
         self._call(stream, lib.lsp_paged_evict, tensor("weights", weights, f32, slots), tensor("pos", pos, i32, slots), tensor("lens", lens, i32, b),
                    tensor("seen", seen, i32, b), budget, n_sink, n_recent, tensor("weights_out", weights_out, f32, slots),
