@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(PP_THREADS, 5) k_paged_append(const PagedAppen
   const int B = a.pv.batch, cap = pg_capacity(a.pv);
   pdl_release();
   pg_prefetch_table(a.pv);
-  pg_prefetch(a.lens, B * 4, threadIdx.x * gridDim.x + blockIdx.x, gridDim.x * PP_THREADS);
+  pg_prefetch_grid(a.lens, B * 4);
   pdl_wait();
   if (blockIdx.x == gridDim.x - 1) {
     bool descend = false;
@@ -356,7 +356,7 @@ __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a
   {
     // (a sequence to thin has more slots than the budget; of the others fewer are read)
     const long long bytes = (long long)min(cap, a.budget) * 4;
-    pg_prefetch(a.lens, a.pv.batch * 4, tid + blockIdx.x * THREADS, gridDim.x * THREADS);
+    pg_prefetch_grid(a.lens, a.pv.batch * 4);
     pg_prefetch(a.weights + base, bytes, tid + rank * THREADS, CL * THREADS);
     if (a.pos) pg_prefetch(a.pos + base, bytes, tid + rank * THREADS, CL * THREADS);
     pg_prefetch_table(a.pv);

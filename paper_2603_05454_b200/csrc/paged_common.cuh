@@ -50,12 +50,17 @@ __device__ __forceinline__ int pg_page(const PagedView& pv, int b, int p) {
   return id;
 }
 // Asks for bytes at p to come to L2 (thread `i` of n, a line each).  Ahead of the wait for a preceding kernel: nothing is read.
-__device__ __forceinline__ void pg_prefetch(const void* p, long long bytes, int i, int n) {
-  for (long long at = (long long)i * 128; p && at < bytes; at += (long long)n * 128) asm volatile("prefetch.global.L2 [%0];" ::"l"((const char*)p + at));
+// (64 bits: a launch may have 2^23 blocks and more, 2^31 threads.)
+__device__ __forceinline__ void pg_prefetch(const void* p, long long bytes, long long i, long long n) {
+  for (long long at = i * 128; p && at < bytes; at += n * 128) asm volatile("prefetch.global.L2 [%0];" ::"l"((const char*)p + at));
+}
+// By the whole grid, neighbouring lines by neighbouring blocks.
+__device__ __forceinline__ void pg_prefetch_grid(const void* p, long long bytes) {
+  pg_prefetch(p, bytes, (long long)threadIdx.x * gridDim.x + blockIdx.x, (long long)gridDim.x * blockDim.x);
 }
 // The page table, a megabyte of it at most, by the whole grid.
 __device__ __forceinline__ void pg_prefetch_table(const PagedView& pv) {
-  pg_prefetch(pv.table, min((long long)pv.batch * pv.max_pages * 4, 1ll << 20), threadIdx.x * gridDim.x + blockIdx.x, gridDim.x * blockDim.x);
+  pg_prefetch_grid(pv.table, min((long long)pv.batch * pv.max_pages * 4, 1ll << 20));
 }
 // Where slot j of sequence b begins (0 <= j < capacity), in elements from the pool's start; -1 where its page is none.
 __device__ __forceinline__ long long pg_slot(const PagedView& pv, int b, int j) {
