@@ -290,7 +290,8 @@ typedef struct {
  *   k_new, v_new   device, packed rows [n_rows] ld_new elements apart, n_kv_heads * head_dim each: sequence b's rows are
  *                  row_off[b] .. row_off[b + 1]  (row_off: device [batch + 1]; NULL: max_rows rows for every sequence, n_rows = batch * max_rows)
  *   max_rows       upper bound of a sequence's rows
- *   lens, lens_out device [batch]; lens_out[b] = lens[b] + rows.  Outputs must not overlap inputs (two buffers, in turn).
+ *   lens, lens_out device [batch]; lens_out[b] = lens[b] + rows.  lens_out and seen_out must not overlap what the call reads (two buffers,
+ *                  in turn).
  *   weights, pos   device [batch][n_kv_heads][max_pages * page_size] or NULL: set to 0 and to the row's position seen[b] + i
  *                  (seen NULL: the slot) in the new slots
  *   seen, seen_out device [batch] or both NULL: positions so far, which after an eviction are more than the slots; seen_out = seen + rows
@@ -305,7 +306,8 @@ int lsp_paged_append(const lsp_paged_kv* kv, const void* k_new, const void* v_ne
  *   lse[r, h] = ln sum_j exp(scale q[r, h] . k_j)               device [n_rows][n_heads], or NULL
  *   weights_out[b, g, j] = weights_in[b, g, j] + sum over the sequence's rows r and the group's heads h of the softmax weight of slot j
  *                                                               device [batch][n_kv_heads][max_pages * page_size], or NULL; weights_in NULL: 0;
- *                                                               may be the same array; slots behind lens[b] are not written
+ *                                                               may be the same array, else not overlapping it; slots behind
+ *                                                               lens[b] are not written
  * A row over no slot (lens[b] = 0), or whose scores are all -inf, gets 0 and lse -inf.  q, out: packed rows as for the append, ldq and ldo
  * elements apart.  The slots are split over the device and the parts joined in a fixed order: the same inputs give the same bits.
  * Accumulation in fp32; bf16 softmax weights enter the product with V as a sum of two.  Meant for up to some dozens of (row, head)

@@ -5,6 +5,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <initializer_list>
 
 #include "../../include/lsp.h"
 #include "paged_attention.cuh"
@@ -74,6 +75,17 @@ bool off_boundary(const P*... p) { return (((uintptr_t)p & 3) | ...); }
 
 bool overlap(const void* a, const void* b, size_t bytes_a, size_t bytes_b) {
   return a && b && (const char*)a < (const char*)b + bytes_b && (const char*)b < (const char*)a + bytes_a;
+}
+struct Array { const void* p; size_t bytes; };
+// An output that overlaps an input or another output (where NULL nothing does).
+bool outputs_overlap(std::initializer_list<Array> outputs, std::initializer_list<Array> inputs) {
+  for (const Array* o = outputs.begin(); o != outputs.end(); ++o) {
+    for (const Array& i : inputs)
+      if (overlap(o->p, i.p, o->bytes, i.bytes)) return true;
+    for (const Array* q = outputs.begin(); q != o; ++q)
+      if (overlap(o->p, q->p, o->bytes, q->bytes)) return true;
+  }
+  return false;
 }
 
 constexpr size_t kCounters = 4096;        // the first bytes of a workspace: arrival counters, 0 between calls
@@ -189,9 +201,8 @@ int lsp_paged_append(const lsp_paged_kv* kv, const void* k_new, const void* v_ne
   if (!lens || !lens_out || (n_rows > 0 && (!k_new || !v_new))) return e.fail(LSP_ERR_ARG, "%s: NULL pointer", who);
   if (off_boundary(lens, row_off, lens_out, weights, pos, seen, seen_out)) return e.fail(LSP_ERR_ARG, "%s: misaligned array", who);
   if ((seen_out != nullptr) != (seen != nullptr)) return e.fail(LSP_ERR_ARG, "%s: seen and seen_out come together", who);
-  const size_t nb = (size_t)kv->batch * 4;
-  if (overlap(lens, lens_out, nb, nb) || overlap(seen, seen_out, nb, nb) || overlap(lens, seen_out, nb, nb) || overlap(seen, lens_out, nb, nb) ||
-      overlap(seen_out, lens_out, nb, nb))
+  const size_t nb = (size_t)kv->batch * 4, nt = nb * kv->max_pages;
+  if (outputs_overlap({{lens_out, nb}, {seen_out, nb}}, {{lens, nb}, {seen, nb}, {row_off, nb + 4}, {kv->page_table, nt}}))
     return e.fail(LSP_ERR_ARG, "%s: lens_out and seen_out must not overlap what the call reads, nor one another", who);
   a.esz = kv->dtype == 0 ? 4 : 2;
   if ((ld_new * a.esz) % 16 || ((uintptr_t)k_new & 15) || ((uintptr_t)v_new & 15) || ld_new < (long long)kv->n_kv_heads * kv->head_dim)
@@ -242,6 +253,9 @@ int lsp_paged_attention(const lsp_paged_kv* kv, const void* q, long long ldq, in
   if (n_heads < 1 || n_heads % kv->n_kv_heads) return e.fail(LSP_ERR_SHAPE, "%s: %d query heads over %d KV heads", who, n_heads, kv->n_kv_heads);
   if (!(scale > 0.f) || std::isinf(scale)) return e.fail(LSP_ERR_ARG, "%s: scale must be positive and finite", who);
   if (weights_in && !weights_out) return e.fail(LSP_ERR_ARG, "%s: weights_in without weights_out", who);
+  const size_t nw = (size_t)kv->batch * kv->n_kv_heads * kv->max_pages * kv->page_size * 4;
+  if (weights_in != weights_out && overlap(weights_in, weights_out, nw, nw))
+    return e.fail(LSP_ERR_ARG, "%s: weights_in and weights_out must be the same array or not overlap", who);
   const int esz = kv->dtype == 0 ? 4 : 2, qd = n_heads * kv->head_dim;
   if ((ldq * esz) % 16 || (ldo * esz) % 16 || ((uintptr_t)q & 15) || ((uintptr_t)out & 15) || ldq < qd || ldo < qd)
     return e.fail(LSP_ERR_ARG, "%s: rows of q and out must be 16-byte aligned and at least n_heads x head_dim elements apart", who);
@@ -306,9 +320,8 @@ int lsp_paged_evict(const lsp_paged_kv* kv, const float* weights, const int32_t*
   if (budget < 1 || n_sink < 0 || n_recent < 0 || (long long)n_sink + n_recent > budget)
     return e.fail(LSP_ERR_ARG, "%s: budget %d must be positive and hold n_sink %d + n_recent %d", who, budget, n_sink, n_recent);
   const long long cap = (long long)kv->max_pages * kv->page_size;
-  const size_t nb = (size_t)kv->batch * 4, nw = (size_t)kv->batch * kv->n_kv_heads * cap * 4;
-  if (overlap(lens, lens_out, nb, nb) || overlap(seen, lens_out, nb, nb) || overlap(weights, weights_out, nw, nw) || overlap(pos, pos_out, nw, nw) ||
-      overlap(weights, pos_out, nw, nw) || overlap(pos, weights_out, nw, nw) || overlap(weights_out, pos_out, nw, nw))
+  const size_t nb = (size_t)kv->batch * 4, nw = nb * kv->n_kv_heads * cap, nt = nb * kv->max_pages;
+  if (outputs_overlap({{weights_out, nw}, {pos_out, nw}, {lens_out, nb}}, {{weights, nw}, {pos, nw}, {lens, nb}, {seen, nb}, {kv->page_table, nt}}))
     return e.fail(LSP_ERR_ARG, "%s: outputs must not overlap what the call reads, nor one another", who);
   if ((uintptr_t)workspace & 255) return e.fail(LSP_ERR_ARG, "%s: the workspace must be 256-byte aligned", who);
   const size_t need = lsp_paged_evict_workspace(kv, budget);
