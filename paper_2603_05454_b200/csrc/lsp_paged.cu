@@ -256,7 +256,8 @@ int lsp_paged_attention(const lsp_paged_kv* kv, const void* q, long long ldq, in
   const size_t nw = (size_t)kv->batch * kv->n_kv_heads * kv->max_pages * kv->page_size * 4;
   if (weights_in != weights_out && overlap(weights_in, weights_out, nw, nw))
     return e.fail(LSP_ERR_ARG, "%s: weights_in and weights_out must be the same array or not overlap", who);
-  const int esz = kv->dtype == 0 ? 4 : 2, qd = n_heads * kv->head_dim;
+  const int esz = kv->dtype == 0 ? 4 : 2;
+  const long long qd = (long long)n_heads * kv->head_dim;
   if ((ldq * esz) % 16 || (ldo * esz) % 16 || ((uintptr_t)q & 15) || ((uintptr_t)out & 15) || ldq < qd || ldo < qd)
     return e.fail(LSP_ERR_ARG, "%s: rows of q and out must be 16-byte aligned and at least n_heads x head_dim elements apart", who);
   if ((uintptr_t)workspace & 255) return e.fail(LSP_ERR_ARG, "%s: the workspace must be 256-byte aligned", who);

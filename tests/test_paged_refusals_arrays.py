@@ -1,4 +1,4 @@
-"""More of what the calls of the paged key-value cache refuse on the host: arrays that overlap what a call reads.  No GPU."""
+"""More of what the calls of the paged key-value cache refuse on the host: arrays that overlap what a call reads, widths beyond 31 bits.  No GPU."""
 import pytest
 
 import test_paged_refusals as R
@@ -35,3 +35,12 @@ def test_weights_in_place_and_arrays_side_by_side_pass():
     per_slot = 2 * 4 * 64 * 4
     assert R._attention(weights_in=12 * P, weights_out=12 * P + per_slot)[0] == WORKSPACE
     assert R._evict(weights_out=10 * P + per_slot, pos_out=11 * P + per_slot, lens_out=6 * P + 8)[0] == WORKSPACE
+
+
+@pytest.mark.parametrize("ld", [dict(ldq=1 << 24), dict(ldo=1 << 24)])
+def test_rows_wider_than_31_bits_of_elements(ld):
+    """2^24 heads of 128: a distance of rows that is smaller than a row is seen."""
+    a = dict(n_heads=1 << 24, max_rows=1, ldq=1 << 31, ldo=1 << 31, workspace_bytes=0)
+    a.update(ld)
+    rc, msg = R._attention(**a)
+    assert rc == ARG and "elements apart" in msg, (rc, msg)
