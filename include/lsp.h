@@ -270,12 +270,13 @@ int lsp_linear_static(const void* A, const void* W, void* out, int M, int N, int
  * sequence b is row j % page_size of page page_table[b * max_pages + j / page_size].  A decoder's own cache plane is the special
  * case without a table.  The calls need no context, allocate nothing, enqueue on cuda_stream (a cudaStream_t; NULL = default
  * stream) of the current device and return; they may be captured into a CUDA graph.  Lengths and tables are device memory, read
- * when the kernels run (more than once: nothing may write them, or what else a call reads, meanwhile).  What only the device sees goes to the status word: bit 1 = a length outside [0, max_pages * page_size],
- * or an append past it (clamped); bit 2 = a table entry outside [0, n_pages) for a slot in use (the slot is not read or written and gets
- * no weight; a pair of slots of an eviction is not moved, and the slot ahead of the budget keeps its own weight and position); bit 4 = row offsets that descend, leave [0, n_rows] or span more
- * than max_rows (that sequence has no rows then).  Nothing outside the given buffers is touched in any of these cases, and the
- * other sequences' results hold (where offsets descend in such a way that two of them name a row, it is appended to both, and its attention
- * and their weights are undefined).  err, err_len: optional host buffer for the message of a failing call.
+ * when the kernels run (more than once: nothing may write them, or what else a call reads, meanwhile).  What only the device sees
+ * goes to the status word: bit 1 = a length outside [0, max_pages * page_size], or an append past it (clamped); bit 2 = a table entry
+ * outside [0, n_pages) for a slot in use (the slot is not read or written and gets no weight; a pair of slots of an eviction is not
+ * moved, and the slot ahead of the budget keeps its own weight and position); bit 4 = row offsets that descend, leave [0, n_rows] or
+ * span more than max_rows (that sequence has no rows then).  Nothing outside the given buffers is touched in any of these cases, and
+ * the other sequences' results hold (where offsets descend in such a way that two of them name a row, it is appended to both, and its
+ * attention and their weights are undefined).  err, err_len: optional host buffer for the message of a failing call.
  * Limits: head_dim 64 or 128, batch <= 1024, n_kv_heads <= 1024, max_pages * page_size <= 2^20, every pointer and stride of T a
  * multiple of 16 bytes. */
 typedef struct {

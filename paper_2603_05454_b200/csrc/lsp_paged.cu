@@ -148,8 +148,9 @@ cudaError_t launch_attention(const PagedAttnArgs& a0, int tiles, cudaStream_t st
   a.lane_bits = tiles > 1 ? PA_LANE_BITS : 0;
   const long long units = (long long)a.pv.batch * a.pv.hkv * ((tiles + (1 << a.lane_bits) - 1) >> a.lane_bits);      // of a lane
   const long long most = ((cap + PA_CHUNK - 1) / PA_CHUNK + PA_UNIT_COST) * units;       // numbers to deal, if every sequence were full
-  // At most 32 runs a unit: one CTA adds the parts.  One sequence of 8000 / 30011 slots of 4 KV heads: 16.0 / 27.4 us, without the bound (74
-  // parts) 21.5 / 30.3, with 16 16.8 / 36.3.
+  // At most 32 times as many runs as units: one CTA adds a unit's parts, 32 of them where the sequences are alike.  One sequence of 8000 / 30011 slots
+  // of 4 KV heads: 16.0 / 27.4 us, without the bound (74 parts) 21.5 / 30.3, with 16 16.8 / 36.3.  (Beside short sequences a long one's units have more
+  // parts: 8000 beside seven of 100 57, 16.3 us where it takes 14.0 alone; 30011 beside seven of 300 66, 22.6 and 23.8.)
   a.n_runs = (int)std::min({most, 32 * units, (long long)std::min(n_per_sm * n_sm, pa_max_ctas(DH)) >> a.lane_bits});
   e = launch_k(1, kern, dim3(a.n_runs << a.lane_bits), dim3(PA_THREADS), (size_t)smem, stream, a);
   if (e != cudaSuccess || !a.scores) return e;
@@ -161,11 +162,13 @@ cudaError_t launch_attention(const PagedAttnArgs& a0, int tiles, cudaStream_t st
                   stream, a, key_blocks);
 }
 
-// Where there are more units than SMs, of at most 4096 slots: a CTA of 256 threads each (four fit an SM), which moves what it selected.  Else CTAs of 1024 threads, a
-// cluster of them per unit while that fills no more than the SMs and leaves each CTA 3000 slots (or where a CTA cannot hold them), and the
-// moves over the whole grid.  Measured, us: 512 units of about 1030 / up to 2047 slots moved by their CTAs 12.4 / 44.8, over the grid 14.2 / 46.8
-// (of 2047 each to 1024 64.4 and 64.3); 16 units of up to 4093 slots without a cluster 12.6, with two CTAs 13.3; 4 units of 30000 slots with
-// eight CTAs 19.1, four 24.0, two 29.4.
+// Where there are more units than SMs, of at most 4096 slots: a CTA of 256 threads each (four fit an SM up to some 3200 slots, three beyond), which
+// moves what it selected.  Else CTAs of 1024 threads, a cluster of them per unit while that fills no more than the SMs and leaves each CTA 3000
+// slots (or where a CTA cannot hold them), and the moves over the whole grid.  `cap`, the table's width, stands for the slots, which only the device
+// knows: a table far wider than its sequences costs time (512 units of about 1030 slots to 1024: tables for 1088 / 4096 slots 9.7 / 9.0 us, 4160 /
+// 8192 22.1, 32768 92).  Measured with tables as wide as the sequences, us: 512 units of about 1030 / up to 2047 slots moved by their CTAs 12.4 /
+// 44.8, over the grid 14.2 / 46.8 (of 2047 each to 1024 64.4 and 64.3); 16 units of up to 4093 slots without a cluster 12.6, with two CTAs
+// 13.3; 4 units of 30000 slots with eight CTAs 19.1, four 24.0, two 29.4.
 cudaError_t launch_evict(PagedEvictArgs& a, int units, int cap, int n_sm, cudaStream_t stream) {
   const bool small = units > n_sm && cap <= 4096;
   a.cluster = 1;

@@ -537,8 +537,8 @@ __device__ __forceinline__ void pa_empty(const PagedAttnArgs& a, const int* pre)
 }
 
 // ---- bf16: tensor cores --------------------------------------------------------------------------------------------------
-// Softmax weights are fed to the P V product as the sum of two bf16 numbers (16 bits of mantissa): the tensor pipe has the time,
-// and the output is then as exact as one with fp32 weights.
+// Softmax weights are fed to the P V product as the sum of two bf16 numbers (16 bits of mantissa): the tensor pipe has the time, and
+// ahead of its rounding the output is within 2e-6 of one with fp32 weights (a last bit of bf16 differs in one element of some 400).
 // The maximum is raised only where a score is more than 2^PA_LAZY times the weight of the present one (the sums have room for that), so that most
 // chunks need neither its exchange over the lanes nor a rescale.
 constexpr float PA_LAZY = 8.f;

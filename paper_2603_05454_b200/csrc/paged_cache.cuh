@@ -383,7 +383,7 @@ __global__ void __launch_bounds__(THREADS) k_paged_select(const PagedEvictArgs a
   auto key_of = [&](int p, float w) { return (p < a.n_sink || p >= seen - a.n_recent) ? 0u : pe_key(w); };
   unsigned any = 0;                                // bits that some position has
   if (a.in_smem) {
-    // four slots a load where a KV head's array begins on 16 bytes (behind the last slot there may be anything up to the next multiple of four)
+    // four slots a load where a KV head's array begins on 16 bytes, the last ones one by one
     const bool by4 = (cap & 3) == 0 && (((uintptr_t)weights | (uintptr_t)pos) & 15) == 0;
     const int ahead4 = by4 ? ns / 4 : 0;
 #pragma unroll 2
