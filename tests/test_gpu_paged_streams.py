@@ -119,6 +119,29 @@ def test_a_stream_from_outside_torch_may_be_gone_before_the_object():
     assert bool((torch.full((n,), 3, dtype=torch.uint8, device=DEV) == 3).all())
 
 
+def test_the_first_call_in_a_capture_and_the_object_dropped_behind_the_graph():
+    pool = _pool()
+    q = torch.randn(2, HEADS[0] * 64, device=DEV).to(BF)
+    want, out, graph = _want(pool, q), torch.zeros_like(q), torch.cuda.CUDAGraph()
+    c = _object(pool)
+    at, n = c.workspace.data_ptr(), c.workspace.numel()
+    with torch.cuda.graph(graph):
+        c.attention(q, pool.lens, out)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    out.zero_()
+    c.attention(q, pool.lens, out)                          # eagerly, on the stream of the construction
+    c.check()
+    assert torch.equal(out, want)
+    del graph, c
+    torch.cuda.synchronize()
+    again = [torch.full((n,), 3, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    assert all(bool((t == 3).all()) for t in again)
+
+
 def test_an_object_made_in_a_capture_is_the_graphs_own():
     """Its clears are replayed with the graph, ahead of the calls on every stream of the capture; an eager call is an error, not a wrong result."""
     pool = _pool()
