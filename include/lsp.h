@@ -328,8 +328,9 @@ int lsp_paged_attention(const lsp_paged_kv* kv, const void* q, long long ldq, in
  * slot's weight and position to weights_out and pos_out.  Which slot holds a key carries no meaning for attention (keys are
  * rotated already); pos_out says which position it is, per KV head.  Sequences of at most budget slots keep theirs.
  *   weights, pos        device [batch][n_kv_heads][max_pages * page_size]; pos NULL: the slot (pos_out may be NULL then)
- *   lens, seen          device [batch]; seen NULL: lens, which is right up to the first eviction only: from then on a sequence has seen more positions than
- *                       it has slots, and without seen ever more of them count as recent, until the newest are dropped in favour of older ones
+ *   lens, seen          device [batch]; seen NULL: lens, which is right up to the first eviction only: from then on a sequence has seen
+ *                       more positions than it has slots, and without seen ever more of them count as recent, until the newest are
+ *                       dropped in favour of older ones
  *   weights_out, pos_out, lens_out   as the inputs, not overlapping them; lens_out = min(lens, budget); slots behind it are not written
  * Pages behind ceil(lens_out / page_size) are free afterwards.  The pages of a sequence that is thinned must belong to it alone.
  * workspace: lsp_paged_evict_workspace() bytes, aligned as above; the attention's may be taken (its counters are left alone). */

@@ -371,14 +371,15 @@ class PagedKVCache:
     k_pool, v_pool: [n_pages, page_size, n_kv_heads, head_dim] CUDA tensors (bfloat16 or float32) with the same strides, heads
     contiguous; any view with 16-byte strides will do, a decoder's own planes among them.  page_table: int32 CUDA tensor [batch, max_pages],
     contiguous; without it page p of sequence b is page b * max_pages + p (batch then tells max_pages = n_pages // batch).
-    All tensors are borrowed; page_table may be rewritten between calls.  The object owns the workspace (for any eviction, and for attention of
-    at most n_rows packed rows, by default max_rows for every sequence; with `weights` for attention that gathers them, 4 bytes for every
-    row, query head and slot of a sequence's pages: 16 x 8 rows of 32 heads over 32768 slots are 0.5 GB) and the status word that check() reads.
-    A call costs the host 8 to 13 us: capture the calls of a step into a graph where they take less on the device.  Calls of one object must not overlap on the device: give each stream, and each captured graph that may run
-    beside others, an object of its own over the same pools.  Every call enqueues on the current stream of the pools' device, or on `stream`.
-    An object is ready for any stream once it is made (the constructor waits for its stream).  One made in a stream capture belongs to that graph: its
-    calls are those of the capture, and others raise.  It may be dropped while calls on torch's streams are still running; keep it for those on an
-    external stream, and for the replays of a graph that holds its calls.
+    All tensors are borrowed; page_table may be rewritten between calls.  The object owns the status word that check() reads and the workspace: for any
+    eviction, and for attention of at most n_rows packed rows, by default max_rows for every sequence; with `weights` for attention that gathers
+    them, 4 bytes for every row, query head and slot of a sequence's pages (16 x 8 rows of 32 heads over 32768 slots: 0.5 GB).
+
+    Every call enqueues on the current stream of the pools' device, or on `stream`.  It costs the host 8 to 13 us: capture a step's calls into a graph where
+    they take less on the device.  Calls of one object must not overlap on the device: give each stream, and each captured graph that may run
+    beside others, an object of its own over the same pools.  An object is ready for any stream once it is made (the constructor waits for its
+    stream).  One made in a stream capture belongs to that graph: its calls are those of the capture, and others raise.  It may be dropped while calls
+    on torch's streams are still running; keep it for those on an external stream, and for the replays of a graph that holds its calls.
     """
 
     def __init__(self, k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: Optional[torch.Tensor] = None, *, n_heads: int,
